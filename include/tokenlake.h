@@ -122,6 +122,14 @@ tl_status tl_pool_append_batch(tl_pool* pool, int32_t n_chains, const int32_t* h
                                const int32_t* new_ptr, const uint64_t* new_ids, const int32_t* row_ptr,
                                const void* k_rows_dev, const void* v_rows_dev, int32_t* new_slots_out, void* stream);
 
+/* Registers what tl_pool_append_batch would -- same arguments, checks and slots, fills grow the same -- and copies nothing:
+ * the rows are written by tl_pool_write_rows or tl_pool_move_rows.  rows_out: host [row_ptr[n_chains]], the pool row
+ * (slot * seg_len + token) of each row of the chains.  Rows behind a slot's fill are left as they are.  The caller
+ * has the rows written on a stream in front of the attention that reads them.  Makes no HIP call. */
+tl_status tl_pool_reserve_batch(tl_pool* pool, int32_t n_chains, const int32_t* has_tail, const uint64_t* tail_ids,
+                                const int32_t* new_ptr, const uint64_t* new_ids, const int32_t* row_ptr, int32_t* new_slots_out,
+                                int32_t* rows_out);
+
 /* Register segments whose KV the caller has already written into the pool memory
  * (no copy; the slots' tails are left as they are).  ids/slots/fills: host, [n].
  * Same id twice or slot taken -> TL_EINVAL, nothing is registered. */
@@ -363,6 +371,65 @@ tl_status tl_fused_attn_static(const tl_pool* pool, tl_plan* plan, const void* q
  * lse_out: device [n_tokens, q_heads] fp32, or NULL.  Tokens of one-pass requests are not written. */
 tl_status tl_merge(tl_plan* plan, const float* out_partial, const float* lse, void* out_dev,
                    int32_t out_is_bf16, float* lse_out, void* stream);
+
+/* ------------------------------------------------------------------------------------
+ * Rows between a layer's projection and the attention: norms of queries and keys for each head, position rotation, writes to
+ * the pool, rows of the pool that move.  Every call enqueues one kernel (several in a row from 2^25 / heads * 8 tokens on) and nothing
+ * else: no allocation, no copy, no state kept, so it may be captured into a HIP graph and runs on any stream.  A call of zero tokens
+ * returns TL_OK at once and looks at no other argument.
+ * ------------------------------------------------------------------------------------ */
+
+/* Position rotation.  Pair i of a head's first rot_dim values -- values i and i + rot_dim / 2, or with `interleaved` not 0 values
+ * 2i and 2i + 1 -- is turned by the angle position * inv_freq[i] and multiplied by `factor` (1, or the magnitude that goes with
+ * stretched frequencies; finite); values from rot_dim on stay.  rot_dim: a multiple of 16 from 16 to 128.
+ * steps_dev: device [rot_dim / 2], what tl_rope_steps makes of the frequencies.  Positions are any 32-bit integers, negative ones
+ * among them; the angle is exact to 2^-32 of a turn at all of them.  Calls take the struct by address and read it before they return. */
+typedef struct tl_rope {
+  const uint64_t* steps_dev;
+  int32_t rot_dim;
+  int32_t interleaved;
+  float factor;
+} tl_rope;
+
+/* steps_out[i] = inv_freq[i] (radians per position) as a fraction of a turn times 2^64, modulo 2^64.  inv_freq, steps_out: host [n];
+ * TL_EINVAL for frequencies that are not finite.  Host arithmetic. */
+tl_status tl_rope_steps(const double* inv_freq, int32_t n, uint64_t* steps_out);
+
+/* Rows of n tokens.  q: [n, q_heads, 128], k and v: [n, kv_heads, 128], device, bf16 if is_bf16 is not 0, else fp32; a token's heads
+ * are head_stride elements apart, tokens row_stride, both of any size and sign (q, k and v may be views into one projection's
+ * output), the 128 values of a head follow each other.  NULL: not there.
+ * q_weight / k_weight: device fp32 [128] or NULL.  Given, each head of q / k is divided by the root of the mean of its squares
+ * plus eps and multiplied by the weight, in front of the rotation; eps: positive, normal, looked at only then.
+ * q_out / k_out / v_out: device, dense [n, heads, 128] bf16, rounded once from fp32; v is not changed but for that.  An
+ * output may be its own input if that is dense bf16; any other overlap of an output is TL_EINVAL. */
+typedef struct tl_qkv {
+  const void *q, *k, *v;
+  int64_t q_row_stride, q_head_stride, k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+  int32_t q_heads, kv_heads;
+  int32_t is_bf16;
+  float eps;
+  const float *q_weight, *k_weight;
+  void *q_out, *k_out, *v_out;
+} tl_qkv;
+
+/* Norms and rotation of queries and keys, values as they are, in one pass, to the dense tensors that the attention calls read.
+ * Any of q, k, v may be NULL with its output; one is there.  rope NULL: no rotation.  pos_dev: device int32 [n_tokens], the
+ * tokens' positions (NULL if nothing is rotated). */
+tl_status tl_rotate_rows(const tl_rope* rope, const tl_qkv* rows, const int32_t* pos_dev, int32_t n_tokens, void* stream);
+
+/* tl_rotate_rows that also writes k and v (both there, kv_heads the pool's) to the pool: token i's to the pool row
+ * pool_rows_dev[i] = slot * seg_len + token (device int32 [n_tokens]; from tl_pool_reserve_batch).  k_out and v_out may be
+ * NULL.  A row outside the pool (-1: a padded batch) is not written, its outputs are.  Rows must differ: of a row named
+ * twice each 16 bytes are either token's.  No input and no output may lie in the pool's slots.  Changes no fill and keeps plans valid. */
+tl_status tl_pool_write_rows(tl_pool* pool, const tl_rope* rope, const tl_qkv* rows, const int32_t* pos_dev, const int32_t* pool_rows_dev,
+                             int32_t n_tokens, void* stream);
+
+/* Copies pool row src_rows_dev[i] to pool row dst_rows_dev[i], its keys turned on by shift_dev[i] positions (the pool then has
+ * them as if they had been written that much later; `factor` is not applied again); values are copied.  A key is rounded to
+ * bf16 once more.  All three: device int32 [n_rows]; rope NULL: a plain copy, shift_dev may be NULL.  An entry with a row outside
+ * the pool is left out.  dst rows must differ from each other and from every src row but their own (src = dst turns in place). */
+tl_status tl_pool_move_rows(tl_pool* pool, const tl_rope* rope, const int32_t* src_rows_dev, const int32_t* dst_rows_dev,
+                            const int32_t* shift_dev, int32_t n_rows, void* stream);
 
 /* Switch for tests (process-wide; both settings compute the same thing).  Returns TL_EINVAL for
  * an unknown knob or a value out of range.  Knob:

@@ -36,6 +36,17 @@ class tl_plan_info(C.Structure):
         ("tile_pairs", C.c_int64), ("item_pairs", C.c_int64), ("n_prior_rows", C.c_int32), ("n_unit_workgroups", C.c_int32)]
 
 
+class tl_rope(C.Structure):
+    _fields_ = [("steps_dev", C.c_void_p), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("factor", C.c_float)]
+
+
+class tl_qkv(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v")] + [
+        (n, C.c_int64) for n in ("q_row_stride", "q_head_stride", "k_row_stride", "k_head_stride", "v_row_stride", "v_head_stride")] + [
+        (n, C.c_int32) for n in ("q_heads", "kv_heads", "is_bf16")] + [("eps", C.c_float)] + [
+        (n, C.c_void_p) for n in ("q_weight", "k_weight", "q_out", "k_out", "v_out")]
+
+
 _lib = None
 
 _P, _I32, _U64, _F32, _F64 = C.c_void_p, C.c_int32, C.c_uint64, C.c_float, C.c_double
@@ -49,6 +60,7 @@ _SIGNATURES = {
     "tl_pool_put": (_I32, [_P, _U64, _P, _P, _I32, _I32, C.POINTER(_I32), _P]),
     "tl_pool_append": (_I32, [_P, _I32, _U64, _P, _I32, _P, _P, _I32, _P, _P]),
     "tl_pool_append_batch": (_I32, [_P, _I32, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "tl_pool_reserve_batch": (_I32, [_P, _I32, _P, _P, _P, _P, _P, _P, _P]),
     "tl_pool_adopt": (_I32, [_P, _P, _P, _P, _I32, _P]),
     "tl_pool_release": (_I32, [_P, _U64]),
     "tl_pool_evict_lru": (_I32, [_P, C.POINTER(_U64)]),
@@ -69,6 +81,10 @@ _SIGNATURES = {
     "tl_merge": (_I32, [_P, _P, _P, _P, _I32, _P, _P]),
     "tl_fused_attn": (_I32, [_P, _P, _P, _P, _P, _F32, _P, _P, _P, _I32, _P, _P]),
     "tl_fused_attn_static": (_I32, [_P, _P, _P, _P, _P, _F32, _P, _P, _P, _I32, _P, _P]),
+    "tl_rope_steps": (_I32, [_P, _I32, _P]),
+    "tl_rotate_rows": (_I32, [_P, _P, _P, _I32, _P]),
+    "tl_pool_write_rows": (_I32, [_P, _P, _P, _P, _P, _I32, _P]),
+    "tl_pool_move_rows": (_I32, [_P, _P, _P, _P, _P, _I32, _P]),
     "tl_model_segment_time": (_I32, [_F64, _F64, _F64, _F64, _F64, _PF64]),
     "tl_model_comm_time": (_I32, [_F64, _F64, _F64, _PF64]),
     "tl_model_segment_threshold": (_I32, [_F64, _F64, _F64, _F64, _F64, _F64, _PF64]),
@@ -208,6 +224,19 @@ def tl_pool_append_batch(pool: int, tail_ids, new_ids, row_counts, k_rows, v_row
                                                _addr(row_ptr), _dev(k_rows), _dev(v_rows), _addr(slots) if has_ids else None,
                                                _stream(stream)))
     return slots
+
+
+def tl_pool_reserve_batch(pool: int, tail_ids, new_ids, row_counts):
+    """The arguments of tl_pool_append_batch without the rows.  Returns (slots of the new ids, pool row of each of the chains' rows)."""
+    n = len(tail_ids)
+    has_tail = np.array([t is not None for t in tail_ids], np.int32)
+    tails = np.array([0 if t is None else int(t) for t in tail_ids], np.uint64)
+    new_ptr, row_ptr = _offsets(list(map(len, new_ids)), n), _offsets(row_counts, n)
+    ids = np.array(list(chain.from_iterable(new_ids)), np.uint64)
+    slots, rows = np.full(len(ids), -1, np.int32), np.full(max(int(row_ptr[-1]), 0), -1, np.int32)
+    _check(load_library().tl_pool_reserve_batch(pool, n, _addr(has_tail), _addr(tails), _addr(new_ptr), _addr(ids) if len(ids) else None,
+                                                _addr(row_ptr), _addr(slots) if len(ids) else None, _addr(rows) if len(rows) else None))
+    return slots, rows
 
 
 def tl_pool_adopt(pool: int, ids, slots, fills, stream=None):
@@ -399,6 +428,143 @@ def tl_merge(plan: int, out_partial, lse, out, out_is_bf16: bool, lse_out=None, 
     _check(load_library().tl_merge(plan, _need(out_partial, "out_partial", n_part, "f32"), _need(lse, "lse", n_plse, "f32"),
                                    _need(out, "out", n_q, "bf16" if out_is_bf16 else "f32"), int(bool(out_is_bf16)),
                                    _need(lse_out, "lse_out", n_lse, "f32"), _stream(stream)))
+
+
+# ---- rows between the projection and the attention -----------------------------------------
+def tl_rope_steps(inv_freq) -> np.ndarray:
+    """uint64 [rot_dim / 2]; what tl_rope_of takes is `torch.from_numpy(steps.view(np.int64))` on the device."""
+    f = _host(inv_freq, np.float64)
+    steps = np.zeros(len(f), np.uint64)
+    _check(load_library().tl_rope_steps(_addr(f) if len(f) else None, len(f), _addr(steps) if len(f) else None))
+    return steps
+
+
+def tl_rope_of(steps, interleaved: bool = False, factor: float = 1.0) -> tl_rope:
+    """steps: int64 device tensor [rot_dim / 2] with the bits of tl_rope_steps; the struct keeps it alive."""
+    at, n = _vector(steps, "steps", "i64", None, None)
+    rope = tl_rope(at, 2 * n, int(bool(interleaved)), factor)
+    rope.steps, rope.device = steps, steps.get_device()
+    return rope
+
+
+_ROW_KINDS = {}
+
+
+def _row_kinds():
+    if not _ROW_KINDS:
+        import torch
+        _ROW_KINDS.update(bf16=torch.bfloat16, f32=torch.float32, i32=torch.int32, i64=torch.int64, current=torch.cuda.current_device)
+    return _ROW_KINDS
+
+
+def _vector(t, name, kind, n, device):
+    """(address, elements) of a dense one-dimensional device tensor of n elements (n None: any number)."""
+    if t.dtype != _row_kinds()[kind]:
+        raise TypeError("%s must be %s, is %s" % (name, kind, t.dtype))
+    dev = t.get_device()
+    if dev < 0 or (device is not None and dev != device):
+        raise ValueError("%s is on another device" % name)
+    m = t.numel()
+    if t.dim() != 1 or (n is not None and m != n) or not t.is_contiguous():
+        raise ValueError("%s must be dense [%s], is %s" % (name, "n" if n is None else n, tuple(t.shape)))
+    return t.data_ptr(), m
+
+
+def _rows3(t, name, dtype, n, device):
+    """(address, tokens, heads, token stride, head stride) of [n, heads, 128]; values of a head follow each other."""
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, is %s" % (name, dtype, t.dtype))
+    if t.get_device() != device:
+        raise ValueError("%s is on another device" % name)
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[2] != 128 or stride[2] != 1 or (n is not None and shape[0] != n):
+        raise ValueError("%s must be [%s, heads, 128] with adjacent values, is %s with strides %s" % (name, "n" if n is None else n, tuple(shape), stride))
+    return t.data_ptr(), shape[0], shape[1], stride[0], stride[1]
+
+
+def _dense3(t, name, n, heads, device):
+    at, _, h, row, head = _rows3(t, name, _ROW_KINDS["bf16"], n, device)
+    if h != heads or not t.is_contiguous():
+        raise ValueError("%s must be dense [%d, %d, 128], is %s with strides %s" % (name, n, heads, tuple(t.shape), t.stride()))
+    return at
+
+
+def _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps):
+    """(rope, tl_qkv, positions, tokens, device) of a call: shapes, types, strides and devices of its tensors are checked here."""
+    kinds = _row_kinds()
+    some = q if q is not None else k if k is not None else v
+    if some is None:
+        raise ValueError("no rows")
+    dtype, device = some.dtype, some.get_device()
+    if device < 0 or device != kinds["current"]():
+        raise ValueError("rows must be on the current device")
+    if dtype != kinds["bf16"] and dtype != kinds["f32"]:
+        raise TypeError("rows must be bf16 or f32, are %s" % dtype)
+    n, qh, kvh = some.shape[0], 0, 0
+    qp = kp = vp = qo = ko = vo = qw = kw = None
+    qr = qs = kr = ks = vr = vs = 0
+    if q is not None:
+        qp, _, qh, qr, qs = _rows3(q, "q", dtype, n, device)
+    if k is not None:
+        kp, _, kvh, kr, ks = _rows3(k, "k", dtype, n, device)
+    if v is not None:
+        vp, _, h, vr, vs = _rows3(v, "v", dtype, n, device)
+        if k is not None and h != kvh:
+            raise ValueError("k has %d heads, v %d" % (kvh, h))
+        kvh = h
+    if q_out is not None:
+        qo = _dense3(q_out, "q_out", n, qh, device)
+    if k_out is not None:
+        ko = _dense3(k_out, "k_out", n, kvh, device)
+    if v_out is not None:
+        vo = _dense3(v_out, "v_out", n, kvh, device)
+    if q_weight is not None:
+        qw = _vector(q_weight, "q_weight", "f32", 128, device)[0]
+    if k_weight is not None:
+        kw = _vector(k_weight, "k_weight", "f32", 128, device)[0]
+    at = None
+    if rope is not None:
+        if rope.device != device:
+            raise ValueError("the rotation's steps are on another device")
+        if pos is not None:
+            at = _vector(pos, "pos", "i32", n, device)[0]
+    return tl_qkv(qp, kp, vp, qr, qs, kr, ks, vr, vs, qh, kvh, dtype == kinds["bf16"], eps, qw, kw, qo, ko, vo), at, n, device
+
+
+def _ref(rope):
+    return None if rope is None else C.byref(rope)
+
+
+def tl_rotate_rows(rope: Optional[tl_rope], pos, q=None, k=None, v=None, q_out=None, k_out=None, v_out=None, q_weight=None, k_weight=None,
+                   eps: float = 1e-6, stream=None):
+    """Norms (with weights) and rotation (with rope) of q [n, q_heads, 128] and k [n, kv_heads, 128] with any strides between tokens and
+    heads, bf16 or fp32; v as it is; to dense bf16 tensors.  pos: int32 [n]."""
+    rows, at, n, _ = _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps)
+    _check(load_library().tl_rotate_rows(_ref(rope), C.byref(rows), at, n, _stream(stream)))
+
+
+def tl_pool_write_rows(pool: int, rope: Optional[tl_rope], pos, pool_rows, k, v, q=None, q_out=None, k_out=None, v_out=None, q_weight=None,
+                       k_weight=None, eps: float = 1e-6, stream=None):
+    """tl_rotate_rows that writes k and v to the pool: token i's to pool row pool_rows[i] (int32 [n], -1: nowhere)."""
+    rows, at, n, device = _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps)
+    _check(load_library().tl_pool_write_rows(pool, _ref(rope), C.byref(rows), at, _vector(pool_rows, "pool_rows", "i32", n, device)[0], n,
+                                             _stream(stream)))
+
+
+def tl_pool_move_rows(pool: int, rope: Optional[tl_rope], src_rows, dst_rows, shift=None, stream=None):
+    """Pool row src_rows[i] to dst_rows[i], keys turned on by shift[i] positions (int32 [n] each)."""
+    src, n = _vector(src_rows, "src_rows", "i32", None, None)
+    device = src_rows.get_device()
+    if device != _row_kinds()["current"]():
+        raise ValueError("rows must be on the current device")
+    dst = _vector(dst_rows, "dst_rows", "i32", n, device)[0]
+    at = None
+    if rope is not None:
+        if rope.device != device:
+            raise ValueError("the rotation's steps are on another device")
+        if shift is not None:
+            at = _vector(shift, "shift", "i32", n, device)[0]
+    _check(load_library().tl_pool_move_rows(pool, _ref(rope), src, dst, at, n, _stream(stream)))
 
 
 def tl_set_option(knob: str, value: int):

@@ -212,20 +212,12 @@ tl_status tl_pool_put(tl_pool* pool, uint64_t segment_id, const void* k_src_dev,
   return TL_OK;
 }
 
-tl_status tl_pool_append_batch(tl_pool* pool, int32_t n_chains, const int32_t* has_tail, const uint64_t* tail_ids,
-                               const int32_t* new_ptr, const uint64_t* new_ids, const int32_t* row_ptr,
-                               const void* k_rows_dev, const void* v_rows_dev, int32_t* new_slots_out, void* stream) {
-  if (!pool || n_chains < 0) TL_FAIL(TL_EINVAL, "tl_pool_append: bad argument");
-  if (n_chains == 0) return TL_OK;
-  if (!has_tail || !new_ptr || !row_ptr) TL_FAIL(TL_EINVAL, "tl_pool_append: null chain arrays");
-  if (new_ptr[0] != 0 || row_ptr[0] != 0) TL_FAIL(TL_EINVAL, "tl_pool_append: offsets must start at 0");
-  for (int32_t c = 0; c < n_chains; ++c) {
-    if (new_ptr[c + 1] < new_ptr[c] || row_ptr[c + 1] < row_ptr[c]) TL_FAIL(TL_EINVAL, "tl_pool_append: offsets must not decrease");
-    if (has_tail[c] && !tail_ids) TL_FAIL(TL_EINVAL, "tl_pool_append: null tail ids");
-  }
+// Validates the chains of `who` and places their rows: fills grow, new ids take slots, and `chunks` says where each run of rows
+// goes.  Nothing changes on error.
+static tl_status place_rows(const char* who, tl_pool* pool, int32_t n_chains, const int32_t* has_tail, const uint64_t* tail_ids,
+                            const int32_t* new_ptr, const uint64_t* new_ids, const int32_t* row_ptr, int32_t* new_slots_out,
+                            std::vector<AppendChunk>& chunks) {
   const int32_t n_new_all = new_ptr[n_chains], n_rows_all = row_ptr[n_chains];
-  if (n_new_all > 0 && !new_ids) TL_FAIL(TL_EINVAL, "tl_pool_append: null new ids");
-  if (n_rows_all > 0 && (!k_rows_dev || !v_rows_dev)) TL_FAIL(TL_EINVAL, "tl_pool_append: null source");
   const int32_t C = pool->seg_len;
   // ---- validate every chain first ----
   std::vector<int32_t> tail_slot(n_chains, -1), room(n_chains, 0);
@@ -236,33 +228,32 @@ tl_status tl_pool_append_batch(tl_pool* pool, int32_t n_chains, const int32_t* h
       if (has_tail[c]) {
         auto it = pool->slot_of.find(tail_ids[c]);
         if (it == pool->slot_of.end())
-          TL_FAIL(TL_ENOTFOUND, "tl_pool_append: tail id %llu not resident", (unsigned long long)tail_ids[c]);
+          TL_FAIL(TL_ENOTFOUND, "%s: tail id %llu not resident", who, (unsigned long long)tail_ids[c]);
         tail_slot[c] = it->second;
         if (pool->refcnt[tail_slot[c]] != 1)
-          TL_FAIL(TL_EINVAL, "tl_pool_append: tail id %llu has %d references, a shared segment does not grow",
+          TL_FAIL(TL_EINVAL, "%s: tail id %llu has %d references, a shared segment does not grow", who,
                   (unsigned long long)tail_ids[c], pool->refcnt[tail_slot[c]]);
         if (n_rows > 0 && !tails.emplace(tail_slot[c], c).second)
-          TL_FAIL(TL_EINVAL, "tl_pool_append: tail id %llu is the tail of two chains", (unsigned long long)tail_ids[c]);
+          TL_FAIL(TL_EINVAL, "%s: tail id %llu is the tail of two chains", who, (unsigned long long)tail_ids[c]);
         room[c] = C - pool->fill[tail_slot[c]];
       }
       const int32_t rest = n_rows > room[c] ? n_rows - room[c] : 0;
       const int32_t need = (rest + C - 1) / C;
       if (n_new != need)
-        TL_FAIL(TL_EINVAL, "tl_pool_append: %d rows need exactly %d new segments, %d given", n_rows, need, n_new);
+        TL_FAIL(TL_EINVAL, "%s: %d rows need exactly %d new segments, %d given", who, n_rows, need, n_new);
     }
     std::unordered_map<uint64_t, int> seen;
     for (int32_t i = 0; i < n_new_all; ++i) {
-      if (pool->slot_of.count(new_ids[i])) TL_FAIL(TL_EINVAL, "tl_pool_append: id %llu already resident", (unsigned long long)new_ids[i]);
-      if (!seen.emplace(new_ids[i], i).second) TL_FAIL(TL_EINVAL, "tl_pool_append: id %llu listed twice", (unsigned long long)new_ids[i]);
+      if (pool->slot_of.count(new_ids[i])) TL_FAIL(TL_EINVAL, "%s: id %llu already resident", who, (unsigned long long)new_ids[i]);
+      if (!seen.emplace(new_ids[i], i).second) TL_FAIL(TL_EINVAL, "%s: id %llu listed twice", who, (unsigned long long)new_ids[i]);
     }
   }
   if (pool->n_slots - pool->n_used < n_new_all)
-    TL_FAIL(TL_EFULL, "tl_pool_append: %d free slots, %d needed", pool->n_slots - pool->n_used, n_new_all);
+    TL_FAIL(TL_EFULL, "%s: %d free slots, %d needed", who, pool->n_slots - pool->n_used, n_new_all);
   if (n_rows_all == 0) return TL_OK;
-  hipStream_t st = (hipStream_t)stream;
 
   // ---- place the rows (host state changes from here on; no failure path below but HIP's) ----
-  std::vector<AppendChunk> chunks;
+  chunks.reserve((size_t)n_chains + n_new_all);
   for (int32_t c = 0; c < n_chains; ++c) {
     const int32_t n_rows = row_ptr[c + 1] - row_ptr[c];
     int32_t row = 0;
@@ -284,6 +275,35 @@ tl_status tl_pool_append_batch(tl_pool* pool, int32_t n_chains, const int32_t* h
       row += n;
     }
   }
+  return TL_OK;
+}
+
+// What can be said of the chains' arrays without the pool.
+static tl_status check_chains(const char* who, int32_t n_chains, const int32_t* has_tail, const uint64_t* tail_ids, const int32_t* new_ptr,
+                              const uint64_t* new_ids, const int32_t* row_ptr) {
+  if (!has_tail || !new_ptr || !row_ptr) TL_FAIL(TL_EINVAL, "%s: null chain arrays", who);
+  if (new_ptr[0] != 0 || row_ptr[0] != 0) TL_FAIL(TL_EINVAL, "%s: offsets must start at 0", who);
+  for (int32_t c = 0; c < n_chains; ++c) {
+    if (new_ptr[c + 1] < new_ptr[c] || row_ptr[c + 1] < row_ptr[c]) TL_FAIL(TL_EINVAL, "%s: offsets must not decrease", who);
+    if (has_tail[c] && !tail_ids) TL_FAIL(TL_EINVAL, "%s: null tail ids", who);
+  }
+  if (new_ptr[n_chains] > 0 && !new_ids) TL_FAIL(TL_EINVAL, "%s: null new ids", who);
+  return TL_OK;
+}
+
+tl_status tl_pool_append_batch(tl_pool* pool, int32_t n_chains, const int32_t* has_tail, const uint64_t* tail_ids,
+                               const int32_t* new_ptr, const uint64_t* new_ids, const int32_t* row_ptr,
+                               const void* k_rows_dev, const void* v_rows_dev, int32_t* new_slots_out, void* stream) {
+  if (!pool || n_chains < 0) TL_FAIL(TL_EINVAL, "tl_pool_append: bad argument");
+  if (n_chains == 0) return TL_OK;
+  tl_status rc = check_chains("tl_pool_append", n_chains, has_tail, tail_ids, new_ptr, new_ids, row_ptr);
+  if (rc != TL_OK) return rc;
+  if (row_ptr[n_chains] > 0 && (!k_rows_dev || !v_rows_dev)) TL_FAIL(TL_EINVAL, "tl_pool_append: null source");
+  const int32_t C = pool->seg_len;
+  hipStream_t st = (hipStream_t)stream;
+  std::vector<AppendChunk> chunks;
+  rc = place_rows("tl_pool_append", pool, n_chains, has_tail, tail_ids, new_ptr, new_ids, row_ptr, new_slots_out, chunks);
+  if (rc != TL_OK || chunks.empty()) return rc;
   const size_t row16 = (size_t)pool->kv_heads * pool->head_dim * 2 / 16;
   const size_t slot16 = row16 * C;
   for (size_t c0 = 0; c0 < chunks.size(); c0 += kAppendChunks) {
@@ -303,6 +323,25 @@ tl_status tl_pool_append_batch(tl_pool* pool, int32_t n_chains, const int32_t* h
   }
   TL_HIP(hipGetLastError());
   return TL_OK;
+}
+
+tl_status tl_pool_reserve_batch(tl_pool* pool, int32_t n_chains, const int32_t* has_tail, const uint64_t* tail_ids,
+                                const int32_t* new_ptr, const uint64_t* new_ids, const int32_t* row_ptr, int32_t* new_slots_out,
+                                int32_t* rows_out) {
+  if (!pool || n_chains < 0) TL_FAIL(TL_EINVAL, "tl_pool_reserve_batch: bad argument");
+  if (n_chains == 0) return TL_OK;
+  tl_status rc = check_chains("tl_pool_reserve_batch", n_chains, has_tail, tail_ids, new_ptr, new_ids, row_ptr);
+  if (rc != TL_OK) return rc;
+  if (row_ptr[n_chains] > 0 && !rows_out) TL_FAIL(TL_EINVAL, "tl_pool_reserve_batch: null rows");
+  try {
+    std::vector<AppendChunk> chunks;
+    rc = place_rows("tl_pool_reserve_batch", pool, n_chains, has_tail, tail_ids, new_ptr, new_ids, row_ptr, new_slots_out, chunks);
+    for (const AppendChunk& c : chunks)
+      for (int32_t i = 0; i < c.n; ++i) rows_out[c.src_row + i] = c.slot * pool->seg_len + c.tok + i;
+  } catch (const std::bad_alloc&) {
+    TL_FAIL(TL_ENOMEM, "tl_pool_reserve_batch: host allocation failed");
+  }
+  return rc;
 }
 
 tl_status tl_pool_append(tl_pool* pool, int32_t has_tail, uint64_t tail_id, const uint64_t* new_ids, int32_t n_new,
