@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from itertools import accumulate, chain
+from struct import Struct
 from typing import Optional
 
 import numpy as np
@@ -441,9 +442,10 @@ def tl_rope_steps(inv_freq) -> np.ndarray:
 
 def tl_rope_of(steps, interleaved: bool = False, factor: float = 1.0) -> tl_rope:
     """steps: int64 device tensor [rot_dim / 2] with the bits of tl_rope_steps; the struct keeps it alive."""
+    _row_kinds()
     at, n = _vector(steps, "steps", "i64", None, None)
     rope = tl_rope(at, 2 * n, int(bool(interleaved)), factor)
-    rope.steps, rope.device = steps, steps.get_device()
+    rope.steps, rope.device, rope.at = steps, steps.get_device(), C.addressof(rope)
     return rope
 
 
@@ -453,86 +455,79 @@ _ROW_KINDS = {}
 def _row_kinds():
     if not _ROW_KINDS:
         import torch
-        _ROW_KINDS.update(bf16=torch.bfloat16, f32=torch.float32, i32=torch.int32, i64=torch.int64, current=torch.cuda.current_device)
+        _ROW_KINDS.update(bf16=torch.bfloat16, f32=torch.float32, i32=torch.int32, i64=torch.int64,
+                          current=getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device))
     return _ROW_KINDS
 
 
 def _vector(t, name, kind, n, device):
     """(address, elements) of a dense one-dimensional device tensor of n elements (n None: any number)."""
-    if t.dtype != _row_kinds()[kind]:
+    if t.dtype is not _ROW_KINDS[kind]:
         raise TypeError("%s must be %s, is %s" % (name, kind, t.dtype))
-    dev = t.get_device()
+    dev, shape = t.get_device(), t.shape
     if dev < 0 or (device is not None and dev != device):
         raise ValueError("%s is on another device" % name)
-    m = t.numel()
-    if t.dim() != 1 or (n is not None and m != n) or not t.is_contiguous():
-        raise ValueError("%s must be dense [%s], is %s" % (name, "n" if n is None else n, tuple(t.shape)))
-    return t.data_ptr(), m
+    if len(shape) != 1 or (n is not None and shape[0] != n) or not t.is_contiguous():
+        raise ValueError("%s must be dense [%s], is %s with strides %s" % (name, "n" if n is None else n, tuple(shape), t.stride()))
+    return t.data_ptr(), shape[0]
 
 
-def _rows3(t, name, dtype, n, device):
-    """(address, tokens, heads, token stride, head stride) of [n, heads, 128]; values of a head follow each other."""
-    if t.dtype != dtype:
-        raise TypeError("%s must be %s, is %s" % (name, dtype, t.dtype))
-    if t.get_device() != device:
-        raise ValueError("%s is on another device" % name)
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or shape[2] != 128 or stride[2] != 1 or (n is not None and shape[0] != n):
-        raise ValueError("%s must be [%s, heads, 128] with adjacent values, is %s with strides %s" % (name, "n" if n is None else n, tuple(shape), stride))
-    return t.data_ptr(), shape[0], shape[1], stride[0], stride[1]
-
-
-def _dense3(t, name, n, heads, device):
-    at, _, h, row, head = _rows3(t, name, _ROW_KINDS["bf16"], n, device)
-    if h != heads or not t.is_contiguous():
-        raise ValueError("%s must be dense [%d, %d, 128], is %s with strides %s" % (name, n, heads, tuple(t.shape), t.stride()))
-    return at
+# tl_qkv as bytes: filling the ctypes structure field by field takes 0.8 us, this 0.2
+_PACK_QKV = Struct("3Q6q3if5Q").pack
 
 
 def _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps):
-    """(rope, tl_qkv, positions, tokens, device) of a call: shapes, types, strides and devices of its tensors are checked here."""
-    kinds = _row_kinds()
+    """(tl_qkv's bytes, positions, tokens, device) of a call: shapes, types, strides and devices of its tensors are checked here."""
+    # (a decoded token's call takes as long here as in the launch: tensors are asked once for what is looked at)
+    kinds = _ROW_KINDS or _row_kinds()
     some = q if q is not None else k if k is not None else v
     if some is None:
         raise ValueError("no rows")
-    dtype, device = some.dtype, some.get_device()
+    dtype, device, bf16 = some.dtype, some.get_device(), kinds["bf16"]
     if device < 0 or device != kinds["current"]():
         raise ValueError("rows must be on the current device")
-    if dtype != kinds["bf16"] and dtype != kinds["f32"]:
+    if dtype is not bf16 and dtype is not kinds["f32"]:
         raise TypeError("rows must be bf16 or f32, are %s" % dtype)
-    n, qh, kvh = some.shape[0], 0, 0
-    qp = kp = vp = qo = ko = vo = qw = kw = None
-    qr = qs = kr = ks = vr = vs = 0
-    if q is not None:
-        qp, _, qh, qr, qs = _rows3(q, "q", dtype, n, device)
-    if k is not None:
-        kp, _, kvh, kr, ks = _rows3(k, "k", dtype, n, device)
-    if v is not None:
-        vp, _, h, vr, vs = _rows3(v, "v", dtype, n, device)
-        if k is not None and h != kvh:
-            raise ValueError("k has %d heads, v %d" % (kvh, h))
-        kvh = h
-    if q_out is not None:
-        qo = _dense3(q_out, "q_out", n, qh, device)
-    if k_out is not None:
-        ko = _dense3(k_out, "k_out", n, kvh, device)
-    if v_out is not None:
-        vo = _dense3(v_out, "v_out", n, kvh, device)
-    if q_weight is not None:
-        qw = _vector(q_weight, "q_weight", "f32", 128, device)[0]
-    if k_weight is not None:
-        kw = _vector(k_weight, "k_weight", "f32", 128, device)[0]
-    at = None
+    n = len(some)
+    at, strides, heads, outs = [], [], [], []
+    for name, x, out in (("q", q, q_out), ("k", k, k_out), ("v", v, v_out)):
+        if x is None:
+            at.append(0)
+            strides += (0, 0)
+            heads.append(0)
+            outs.append(0 if out is None else out.data_ptr())         # (refused by the library)
+            continue
+        shape, stride = x.shape, x.stride()
+        if x.dtype is not dtype:
+            raise TypeError("%s must be %s, is %s" % (name, dtype, x.dtype))
+        if x.get_device() != device:
+            raise ValueError("%s is on another device" % name)
+        if len(shape) != 3 or shape[2] != 128 or stride[2] != 1 or shape[0] != n:
+            raise ValueError("%s must be [%d, heads, 128] with adjacent values, is %s with strides %s" % (name, n, tuple(shape), stride))
+        at.append(x.data_ptr())
+        strides += stride[:2]
+        heads.append(shape[1])
+        if out is None:
+            outs.append(0)
+            continue
+        if out.dtype is not bf16:
+            raise TypeError("%s_out must be bf16, is %s" % (name, out.dtype))
+        if out.get_device() != device:
+            raise ValueError("%s_out is on another device" % name)
+        if out.shape != shape or not out.is_contiguous():
+            raise ValueError("%s_out must be dense %s, is %s with strides %s" % (name, tuple(shape), tuple(out.shape), out.stride()))
+        outs.append(out.data_ptr())
+    if k is not None and v is not None and heads[1] != heads[2]:
+        raise ValueError("k has %d heads, v %d" % (heads[1], heads[2]))
+    qw = 0 if q_weight is None else _vector(q_weight, "q_weight", "f32", 128, device)[0]
+    kw = 0 if k_weight is None else _vector(k_weight, "k_weight", "f32", 128, device)[0]
+    where = None
     if rope is not None:
         if rope.device != device:
             raise ValueError("the rotation's steps are on another device")
         if pos is not None:
-            at = _vector(pos, "pos", "i32", n, device)[0]
-    return tl_qkv(qp, kp, vp, qr, qs, kr, ks, vr, vs, qh, kvh, dtype == kinds["bf16"], eps, qw, kw, qo, ko, vo), at, n, device
-
-
-def _ref(rope):
-    return None if rope is None else C.byref(rope)
+            where = _vector(pos, "pos", "i32", n, device)[0]
+    return _PACK_QKV(*at, *strides, heads[0], heads[1] or heads[2], dtype is bf16, eps, qw, kw, *outs), where, n, device
 
 
 def tl_rotate_rows(rope: Optional[tl_rope], pos, q=None, k=None, v=None, q_out=None, k_out=None, v_out=None, q_weight=None, k_weight=None,
@@ -540,22 +535,23 @@ def tl_rotate_rows(rope: Optional[tl_rope], pos, q=None, k=None, v=None, q_out=N
     """Norms (with weights) and rotation (with rope) of q [n, q_heads, 128] and k [n, kv_heads, 128] with any strides between tokens and
     heads, bf16 or fp32; v as it is; to dense bf16 tensors.  pos: int32 [n]."""
     rows, at, n, _ = _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps)
-    _check(load_library().tl_rotate_rows(_ref(rope), C.byref(rows), at, n, _stream(stream)))
+    _check(load_library().tl_rotate_rows(rope and rope.at, rows, at, n, _stream(stream)))
 
 
 def tl_pool_write_rows(pool: int, rope: Optional[tl_rope], pos, pool_rows, k, v, q=None, q_out=None, k_out=None, v_out=None, q_weight=None,
                        k_weight=None, eps: float = 1e-6, stream=None):
     """tl_rotate_rows that writes k and v to the pool: token i's to pool row pool_rows[i] (int32 [n], -1: nowhere)."""
     rows, at, n, device = _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps)
-    _check(load_library().tl_pool_write_rows(pool, _ref(rope), C.byref(rows), at, _vector(pool_rows, "pool_rows", "i32", n, device)[0], n,
+    _check(load_library().tl_pool_write_rows(pool, rope and rope.at, rows, at, _vector(pool_rows, "pool_rows", "i32", n, device)[0], n,
                                              _stream(stream)))
 
 
 def tl_pool_move_rows(pool: int, rope: Optional[tl_rope], src_rows, dst_rows, shift=None, stream=None):
     """Pool row src_rows[i] to dst_rows[i], keys turned on by shift[i] positions (int32 [n] each)."""
+    kinds = _ROW_KINDS or _row_kinds()
     src, n = _vector(src_rows, "src_rows", "i32", None, None)
     device = src_rows.get_device()
-    if device != _row_kinds()["current"]():
+    if device != kinds["current"]():
         raise ValueError("rows must be on the current device")
     dst = _vector(dst_rows, "dst_rows", "i32", n, device)[0]
     at = None
@@ -564,7 +560,7 @@ def tl_pool_move_rows(pool: int, rope: Optional[tl_rope], src_rows, dst_rows, sh
             raise ValueError("the rotation's steps are on another device")
         if shift is not None:
             at = _vector(shift, "shift", "i32", n, device)[0]
-    _check(load_library().tl_pool_move_rows(pool, _ref(rope), src, dst, at, n, _stream(stream)))
+    _check(load_library().tl_pool_move_rows(pool, rope and rope.at, src, dst, at, n, _stream(stream)))
 
 
 def tl_set_option(knob: str, value: int):

@@ -5,10 +5,15 @@
 //   norm      y = x w / sqrt(mean(x^2) + eps)
 //   rotation  pair (a, b) of frequency f at position p: a' = m (a cos pf - b sin pf), b' = m (a sin pf + b cos pf)
 // rounded once, to bf16, at the end.  The angle is never a float: f / 2 pi is a 64-bit fraction of a turn, and p times it modulo
-// 2^64 is the phase of every 32-bit position of either sign to 2^-33 of a turn, without a table.
+// 2^64 is the phase of every 32-bit position of either sign to 2^-32 of a turn, without a table.
 //
 // What bounds it: every value is read once and written once, about ten operations each, so HBM, and at a few tokens the launch.
+// A wave is 8 heads of one token (8192 tokens of 32/8 heads with norms, 201 MB: 34.2 us, 5.9 TB/s; a copy of as many bytes by a
+// library 38; the 58.5 us of waves that computed all cosines in every lane were the vector unit's).  Waves that take two or four
+// times as many heads share a cosine with more of them and wait longer: 0 to 3 % slower from 20 MB on, 0.3 us at a token;
+// a workgroup that shares them across its waves 5 to 20 % slower, for its barrier.
 #include <cmath>
+#include <type_traits>
 
 #include "attn_common.h"
 
@@ -17,38 +22,61 @@ namespace tl {
 constexpr int kRowThreads = 256;
 constexpr int kMostHeads = 1 << 16;
 constexpr int kWaveHeads = 8;            // heads that a wave takes at once: 8 lanes with 16 values each to a head
+constexpr int kMostTokensLog2 = 3;       // tokens that a wave has
+// What a call moves decides whether the 256 MB of cache in front of HBM are to keep it.  From 104 MiB on what is read makes room for
+// what is written; from 256 MiB on neither would be there when the attention reads it.  Between a producer and a reader of
+// all rows, with neither / loads / both passing by the cache: 67 MB 45.5 / 45.7 / 50 us, 134 MB 93.8 / 90.7 / 84, 201 MB 106 / 101 / 110,
+// 258 MB 150 / 131 / 135, 302 MB 182 / 157 / 155, 470 MB 253 / 266 / 236; alone 14.4 / 16.3 / 14.3, 29 / 27 / 25, 38.8 / 36.8 / 35.2, 48 / 48 / 44,
+// 55 / 55 / 51, 84 / 87 / 79.
+constexpr int64_t kStreamIn = (int64_t)104 << 20, kStreamAll = (int64_t)256 << 20;
 
-struct RowsArgs {
-  const char *q, *k, *v;                 // null: not there
-  int64_t q_row, q_head, k_row, k_head, v_row, v_head;   // strides in bytes
-  uint16_t *q_out, *k_out, *v_out;       // dense, or null
-  uint16_t *pool_k, *pool_v;
-  const int32_t* pool_rows;
-  const float *q_weight, *k_weight;      // null: no norm
-  const int32_t* pos;
-  const uint64_t* steps;                 // null: no rotation
-  float eps, factor;
-  int32_t n_pool_rows;
-  int32_t q_heads, k_heads, heads;       // heads = all that a token has, in the order q, k, v
-  int32_t rot_lanes, interleaved;        // rot_lanes = rot_dim / 16: lanes of a head whose values turn
-  uint32_t first, n_waves, wave_blocks;  // wave_blocks = waves that a token has
+enum { kDense = 0, kToPool = 1, kMove = 2 };      // where rows come from and go to
+enum { kQ = 0, kK = 1, kV = 2 };
+
+// A quotient by a number that the host knows: n / d = n * magic >> 32 for n d < 2^32.
+struct Div {
+  uint32_t d, magic;
+};
+__device__ __forceinline__ uint32_t div_by(uint32_t n, Div x) { return x.d == 1 ? n : __umulhi(n, x.magic); }
+
+// How the heads of one kind are dealt to waves.  A wave takes 8 heads: of one token or, where there are at most 4 (2, 1), of 2 (4, 8) tokens.
+struct Deal {
+  int32_t heads, tokens_log2, waves;     // waves: that the tokens of a group have for this kind
+  Div per_tokens;                        // waves of 1 << tokens_log2 tokens
 };
 
-struct MoveArgs {
-  uint16_t *pool_k, *pool_v;
-  const int32_t *src, *dst, *shift;
+struct RowsArgs {
+  const char* in[3];                     // queries, keys, values (kMove: the pool's keys and values)
+  int64_t row[3], head[3];               // strides in bytes
+  uint16_t* out[3];                      // dense, or null
+  uint16_t* pool[3];                     // kToPool, kMove: where the rows named by dst go
+  const float* weight[3];                // null: no norm
+  Deal deal[3];
+  const int32_t *src, *dst;              // rows of the pool; src: kMove
+  const int32_t* pos;                    // positions (kMove: by how many they move)
   const uint64_t* steps;
-  int32_t n_pool_rows, kv_heads, rot_lanes, interleaved;
-  uint32_t first, n_waves, wave_blocks;
+  float eps, factor;
+  int32_t n_pool_rows;
+  int32_t rot_lanes;                     // rot_dim / 16: lanes of a head whose values turn; 0: no rotation
+  int32_t group_log2;                    // tokens that waves are counted for
+  Div group_waves;
+  uint32_t n_waves;
+  int64_t first, end;                    // tokens of this launch
 };
 
 // 16 bytes from or to any address
+typedef unsigned any_u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+template <bool STREAM>
 __device__ __forceinline__ uint4 get16(const char* p) {
-  uint4 x;
-  __builtin_memcpy(&x, p, sizeof(x));
-  return x;
+  return __builtin_bit_cast(uint4, STREAM ? __builtin_nontemporal_load((const any_u32x4*)p) : *(const any_u32x4*)p);
 }
-__device__ __forceinline__ void put16(uint16_t* p, uint4 x) { __builtin_memcpy(p, &x, sizeof(x)); }
+template <bool STREAM>
+__device__ __forceinline__ void put16(uint16_t* p, uint4 x) {
+  if (STREAM)
+    __builtin_nontemporal_store(__builtin_bit_cast(any_u32x4, x), (any_u32x4*)p);
+  else
+    *(any_u32x4*)p = __builtin_bit_cast(any_u32x4, x);
+}
 
 __device__ __forceinline__ void widen(uint4 u, float* x) {
   const unsigned w[4] = {u.x, u.y, u.z, u.w};
@@ -56,6 +84,11 @@ __device__ __forceinline__ void widen(uint4 u, float* x) {
     x[2 * i] = __builtin_bit_cast(float, w[i] << 16);
     x[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xffff0000u);
   }
+}
+__device__ __forceinline__ float add_square_pair(float acc, unsigned pair) {       // acc + both squares of a packed pair of bf16
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  const bf16x2_t x = __builtin_bit_cast(bf16x2_t, pair);
+  return __builtin_amdgcn_fdot2_f32_bf16(x, x, acc, false);
 }
 __device__ __forceinline__ uint4 narrow(const float* x) {
   return __builtin_bit_cast(uint4, pack_bf16x8(x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]));
@@ -84,14 +117,63 @@ __device__ __forceinline__ float sum8(float x) {
   return dpp_add<0x141>(dpp_add<0x4e>(dpp_add<0xb1>(x)));   // lanes 1 apart, 2 apart, and the other four by a mirrored half row
 }
 
-// x[16] of the lane, normed.  A sum of squares beyond 32 bits (rows that large mean something is wrong upstream, but their norm
-// is an ordinary number) is taken again of the values times 2^-70.
-__device__ __forceinline__ void norm16(float* x, float eps, const float* w0, const float* w1) {
+// Where the two runs of 8 values of lane l of a head begin.  Lanes whose values turn against each other from afar (i with
+// i + rot_dim / 2) hold one run of each half of the turning dimensions, so that both of a pair are in one lane; others 16 in a row.
+__device__ __forceinline__ int2 runs_of(int l, int rot_lanes, bool interleaved) {
+  return !interleaved && l < rot_lanes ? make_int2(8 * l, 8 * (rot_lanes + l)) : make_int2(16 * l, 16 * l + 8);
+}
+
+// A lane's 16 values as they are in memory, two runs of 8.
+template <bool BF16>
+struct Lane16 {
+  uint4 u[BF16 ? 2 : 4];
+  template <bool STREAM>
+  __device__ __forceinline__ void load(const char* p, int2 at) {
+    const char *x = p + (BF16 ? 2 : 4) * at.x, *y = p + (BF16 ? 2 : 4) * at.y;
+    if (BF16) {
+      u[0] = get16<STREAM>(x);
+      u[1] = get16<STREAM>(y);
+    } else {
+      u[0] = get16<STREAM>(x);
+      u[1] = get16<STREAM>(x + 16);
+      u[2] = get16<STREAM>(y);
+      u[3] = get16<STREAM>(y + 16);
+    }
+  }
+  __device__ __forceinline__ void values(float* x) const {
+    if (BF16) {
+      widen(u[0], x);
+      widen(u[1], x + 8);
+    } else {
+      __builtin_memcpy(x, u, 64);
+    }
+  }
+};
+
+// Sum of the squares of a head, to each of its 8 lanes.
+template <bool BF16>
+__device__ __forceinline__ float squares(const Lane16<BF16>& raw, const float* x) {
   float ss = 0;
-  for (int i = 0; i < 16; ++i) ss += x[i] * x[i];
-  ss = sum8(ss);
+  if (BF16) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      ss = add_square_pair(add_square_pair(add_square_pair(add_square_pair(ss, raw.u[i].x), raw.u[i].y), raw.u[i].z), raw.u[i].w);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) ss += x[i] * x[i];
+  }
+  return sum8(ss);
+}
+
+// The lane's 16 values over the root of the mean of the head's squares plus eps, times the lane's weights.
+template <bool BF16>
+__device__ __forceinline__ void norm16(const Lane16<BF16>& raw, float* x, float eps, const float* w) {
+  float ss = squares(raw, x);
+  // A sum of squares beyond 32 bits (rows that large mean that something is wrong upstream, but their norm is an ordinary number)
+  // is taken again of the values times 2^-70.
   if (__builtin_expect(ss > 3.4e38f, 0)) {
     ss = 0;
+#pragma unroll
     for (int i = 0; i < 16; ++i) {
       x[i] *= 0x1p-70f;
       ss += x[i] * x[i];
@@ -100,157 +182,170 @@ __device__ __forceinline__ void norm16(float* x, float eps, const float* w0, con
     eps = 0;
   }
   const float r = __builtin_amdgcn_rsqf(ss * (1.f / kHeadDim) + eps);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] *= r * w[i];
+}
+
+// The lane's 8 pairs turned; cs: cosine and sine of pairs 2 j and 2 j + 1 in cs[j].
+template <bool INTER>
+__device__ __forceinline__ void turn16(float* x, const float4* cs) {
+#pragma unroll
   for (int i = 0; i < 8; ++i) {
-    x[i] = x[i] * r * w0[i];
-    x[8 + i] = x[8 + i] * r * w1[i];
+    float &a = x[INTER ? 2 * i : i], &b = x[INTER ? 2 * i + 1 : 8 + i];
+    const float c = i & 1 ? cs[i / 2].z : cs[i / 2].x, s = i & 1 ? cs[i / 2].w : cs[i / 2].y;
+    const float u = a * c - b * s;
+    b = a * s + b * c;
+    a = u;
   }
 }
 
-// x[16] of the lane, turned: pairs 8 l .. 8 l + 7 of the head, c and s theirs.
-__device__ __forceinline__ void turn16(float* x, bool interleaved, const float* c, const float* s) {
-  if (interleaved) {
-    for (int i = 0; i < 8; ++i) {
-      const float a = x[2 * i], b = x[2 * i + 1];
-      x[2 * i] = a * c[i] - b * s[i];
-      x[2 * i + 1] = a * s[i] + b * c[i];
-    }
-  } else {
-    for (int i = 0; i < 8; ++i) {
-      const float a = x[i], b = x[8 + i];
-      x[i] = a * c[i] - b * s[i];
-      x[8 + i] = a * s[i] + b * c[i];
-    }
-  }
-}
-
-// Where the two runs of 8 values of lane l of a head begin.  Lanes whose values turn against each other from afar (i with
-// i + rot_dim / 2) hold one run of each half of the turning dimensions, so that both of a pair are in one lane; others 16 in a row.
-__device__ __forceinline__ int2 runs_of(int l, int rot_lanes, int interleaved) {
-  return !interleaved && l < rot_lanes ? make_int2(8 * l, 8 * (rot_lanes + l)) : make_int2(16 * l, 16 * l + 8);
-}
-
-__device__ __forceinline__ void cos_sin8(const uint64_t* steps, int l, int64_t p, float factor, float* c, float* s) {
-  for (int i = 0; i < 8; ++i) {
-    cos_sin((uint64_t)p * steps[8 * l + i], c[i], s[i]);
-    c[i] *= factor;
-    s[i] *= factor;
-  }
-}
-
-// One wave: 8 heads of one token.
-template <bool BF16, bool TO_POOL>
-__global__ __launch_bounds__(kRowThreads) void rotate_rows_kernel(const RowsArgs a) {
-  const uint32_t wave = blockIdx.x * (kRowThreads / 64) + threadIdx.x / 64;
+// One wave: 8 heads of one kind.  Its lanes compute the cosines and sines of the tokens' positions, a pair each, and hand them over
+// through LDS.  The loads go out first, what is small and wanted first in front.
+template <int MODE, bool BF16, bool INTER, int STREAM>
+__global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
+  constexpr bool kStreamLoads = STREAM >= 1, kStreamStores = STREAM >= 2;
+  extern __shared__ float4 lds_cs[][4][8];              // [wave and token][pairs 8 l + 2 j and the next: j][l]
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * (blockDim.x / 64) + threadIdx.x / 64);
   if (wave >= a.n_waves) return;
-  const uint32_t in_launch = wave / a.wave_blocks;
-  const int64_t token = (int64_t)a.first + in_launch;
-  const int lane = threadIdx.x & 63, l = lane & 7;
-  int h = (int)(wave - in_launch * a.wave_blocks) * kWaveHeads + lane / 8;
-  if (h >= a.heads) return;
-  const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + a.k_heads;
-  const char* src;
-  uint16_t *out, *slots = nullptr;
-  const float* weight = nullptr;
-  int64_t out_row;
-  if (is_q) {
-    src = a.q + token * a.q_row + h * a.q_head;
-    out = a.q_out;
-    out_row = a.q_heads;
-    weight = a.q_weight;
-  } else {
-    h -= a.q_heads;
-    out_row = a.k_heads ? a.k_heads : a.heads - a.q_heads;
-    if (!is_v) {
-      src = a.k + token * a.k_row + h * a.k_head;
-      out = a.k_out;
-      slots = a.pool_k;
-      weight = a.k_weight;
-    } else {
-      h -= a.k_heads;
-      src = a.v + token * a.v_row + h * a.v_head;
-      out = a.v_out;
-      slots = a.pool_v;
+  const uint32_t group = div_by(wave, a.group_waves);
+  uint32_t part = wave - group * a.group_waves.d;
+  int kind = kQ;
+  if (part >= (uint32_t)a.deal[kQ].waves) {
+    part -= a.deal[kQ].waves;
+    kind = kK;
+    if (part >= (uint32_t)a.deal[kK].waves) {
+      part -= a.deal[kK].waves;
+      kind = kV;
     }
   }
-  const int2 at = runs_of(l, a.steps ? a.rot_lanes : 0, a.interleaved);
+  const Deal deal = a.deal[kind];
+  const uint32_t tg = div_by(part, deal.per_tokens);
+  const int at_once = kWaveHeads >> deal.tokens_log2;
+  const int64_t token0 = a.first + ((int64_t)group << a.group_log2) + ((int64_t)tg << deal.tokens_log2);
+  if (token0 >= a.end) return;
+  const int tokens = (int)min((int64_t)1 << deal.tokens_log2, a.end - token0);
+  const int h0 = (int)(part - tg * deal.per_tokens.d) * at_once;
+
+  const int lane = threadIdx.x & 63, l = lane & 7;
+  const int sub = (lane >> 3) >> (3 - deal.tokens_log2), g = (lane >> 3) & (at_once - 1);      // token and head of the lane
+  const bool there = sub < tokens && h0 + g < deal.heads;
+  const int2 at = runs_of(l, a.rot_lanes, INTER);
+  const float* weight = MODE == kMove ? nullptr : a.weight[kind];
+  const bool any_turn = a.rot_lanes && kind != kV, turns = any_turn && l < a.rot_lanes;
+
+  uint64_t step = 0;
+  if (any_turn && lane < 8 * a.rot_lanes) step = a.steps[lane];
+  int32_t row_in = 0, row_out = -1;
+  if (MODE != kDense && deal.tokens_log2 == 0) {             // (by scalar loads)
+    if (MODE == kMove) row_in = a.src[token0];
+    if (kind != kQ) row_out = a.dst[token0];
+  } else if (MODE != kDense && there) {
+    if (MODE == kMove) row_in = a.src[token0 + sub];
+    if (kind != kQ) row_out = a.dst[token0 + sub];
+  }
+  float w[16];
+  if (weight) {
+    __builtin_memcpy(w, weight + at.x, 32);
+    __builtin_memcpy(w + 8, weight + at.y, 32);
+  }
+  if (MODE == kMove && (uint32_t)row_in >= (uint32_t)a.n_pool_rows) row_in = 0, row_out = -1;
+  Lane16<BF16> raw;
+  if (there) {
+    const char* in = a.in[kind] + h0 * a.head[kind] + g * a.head[kind];
+    raw.template load<kStreamLoads>(in + (MODE == kMove ? row_in * a.row[kind] : token0 * a.row[kind] + sub * a.row[kind]), at);
+  }
+
+  auto* const mine = lds_cs + ((threadIdx.x / 64) << a.group_log2);
+  if (any_turn) {
+    for (int i = 0; i < tokens; ++i) {
+      float c, s;
+      cos_sin((uint64_t)(int64_t)a.pos[token0 + i] * step, c, s);
+      ((float2*)&mine[i][(lane >> 1) & 3][lane >> 3])[lane & 1] = make_float2(c * a.factor, s * a.factor);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  }
+  if (!there) return;
   uint4 lo, hi;
-  if (is_v && BF16) {                       // values keep their bits
-    lo = get16(src + 2 * at.x);
-    hi = get16(src + 2 * at.y);
+  if (BF16 && !weight && !any_turn) {       // values keep their bits
+    lo = raw.u[0];
+    hi = raw.u[1];
   } else {
     float x[16];
-    if (BF16) {
-      widen(get16(src + 2 * at.x), x);
-      widen(get16(src + 2 * at.y), x + 8);
+    raw.values(x);
+    if (weight) norm16(raw, x, a.eps, w);
+    if (turns) {
+      float4 cs[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) cs[j] = mine[sub][j][l];
+      turn16<INTER>(x, cs);
+      lo = narrow(x);
+      hi = narrow(x + 8);
     } else {
-      for (int i = 0; i < 2; ++i) {
-        __builtin_memcpy(x + 4 * i, src + 4 * at.x + 16 * i, 16);
-        __builtin_memcpy(x + 8 + 4 * i, src + 4 * at.y + 16 * i, 16);
-      }
+      lo = narrow(x);
+      hi = narrow(x + 8);
     }
-    if (weight) {
-      float w0[8], w1[8];
-      for (int i = 0; i < 8; ++i) w0[i] = weight[at.x + i], w1[i] = weight[at.y + i];
-      norm16(x, a.eps, w0, w1);
-    }
-    if (!is_v && a.steps && l < a.rot_lanes) {
-      float c[8], s[8];
-      cos_sin8(a.steps, l, a.pos[token], a.factor, c, s);
-      turn16(x, a.interleaved, c, s);
-    }
-    lo = narrow(x);
-    hi = narrow(x + 8);
   }
-  if (out) {
-    uint16_t* p = out + (token * out_row + h) * kHeadDim;
-    put16(p + at.x, lo);
-    put16(p + at.y, hi);
+  if (MODE != kMove && a.out[kind]) {
+    uint16_t* p = a.out[kind] + ((token0 + sub) * deal.heads + h0 + g) * kHeadDim;
+    put16<kStreamStores>(p + at.x, lo);
+    put16<kStreamStores>(p + at.y, hi);
   }
-  if (TO_POOL && slots) {
-    const int32_t row = a.pool_rows[token];
-    if ((uint32_t)row < (uint32_t)a.n_pool_rows) {
-      uint16_t* p = slots + ((int64_t)row * out_row + h) * kHeadDim;
-      put16(p + at.x, lo);
-      put16(p + at.y, hi);
-    }
+  if (MODE != kDense && (uint32_t)row_out < (uint32_t)a.n_pool_rows) {
+    uint16_t* p = a.pool[kind] + ((int64_t)row_out * deal.heads + h0 + g) * kHeadDim;
+    put16<kStreamStores>(p + at.x, lo);
+    put16<kStreamStores>(p + at.y, hi);
   }
 }
 
-// One wave: 8 of a pool row's 2 kv_heads heads, keys first.
-__global__ __launch_bounds__(kRowThreads) void move_rows_kernel(const MoveArgs a) {
-  const uint32_t wave = blockIdx.x * (kRowThreads / 64) + threadIdx.x / 64;
-  if (wave >= a.n_waves) return;
-  const uint32_t in_launch = wave / a.wave_blocks;
-  const int64_t entry = (int64_t)a.first + in_launch;
-  const int lane = threadIdx.x & 63, l = lane & 7;
-  int h = (int)(wave - in_launch * a.wave_blocks) * kWaveHeads + lane / 8;
-  if (h >= 2 * a.kv_heads) return;
-  const bool is_v = h >= a.kv_heads;
-  if (is_v) h -= a.kv_heads;
-  const int32_t src = a.src[entry], dst = a.dst[entry];
-  if ((uint32_t)src >= (uint32_t)a.n_pool_rows || (uint32_t)dst >= (uint32_t)a.n_pool_rows) return;
-  uint16_t* pool = is_v ? a.pool_v : a.pool_k;
-  const uint16_t* from = pool + ((int64_t)src * a.kv_heads + h) * kHeadDim;
-  uint16_t* to = pool + ((int64_t)dst * a.kv_heads + h) * kHeadDim;
-  const int2 at = runs_of(l, a.steps ? a.rot_lanes : 0, a.interleaved);
-  uint4 lo = get16((const char*)(from + at.x)), hi = get16((const char*)(from + at.y));
-  if (!is_v && a.steps && l < a.rot_lanes) {
-    float x[16], c[8], s[8];
-    widen(lo, x);
-    widen(hi, x + 8);
-    cos_sin8(a.steps, l, a.shift[entry], 1.f, c, s);
-    turn16(x, a.interleaved, c, s);
-    lo = narrow(x);
-    hi = narrow(x + 8);
-  }
-  put16(to + at.x, lo);
-  put16(to + at.y, hi);
-}
+static Div div_of(uint32_t d) { return {d, d == 1 ? 0u : (uint32_t)(((uint64_t)1 << 32) / d) + 1u}; }
 
-// Tokens of one launch: the grid stays below 2^31 threads and wave numbers below 2^26.
-static uint32_t launch_tokens(uint32_t wave_blocks) {
-  const uint32_t n = (1u << 25) / wave_blocks;
-  return n ? n : 1;
+// Deals the heads of queries, keys and values and launches; `bytes`: what the call reads and writes.
+template <int MODE>
+static tl_status launch(RowsArgs& a, const int32_t (&heads)[3], int32_t n, bool bf16, bool interleaved, int64_t bytes, hipStream_t stream) {
+  a.group_log2 = 0;
+  for (int i = 0; i < 3; ++i) {
+    Deal& d = a.deal[i];
+    d.heads = heads[i];
+    d.tokens_log2 = 0;
+    while (heads[i] && d.tokens_log2 < kMostTokensLog2 && heads[i] << (d.tokens_log2 + 1) <= kWaveHeads) ++d.tokens_log2;
+    if (d.tokens_log2 > a.group_log2) a.group_log2 = d.tokens_log2;
+  }
+  uint32_t waves = 0;
+  for (int i = 0; i < 3; ++i) {
+    Deal& d = a.deal[i];
+    const int32_t at_once = kWaveHeads >> d.tokens_log2;
+    const uint32_t per = heads[i] ? (uint32_t)(heads[i] + at_once - 1) / at_once : 1;
+    d.per_tokens = div_of(per);
+    d.waves = heads[i] ? (int32_t)(per << (a.group_log2 - d.tokens_log2)) : 0;
+    waves += d.waves;
+  }
+  a.group_waves = div_of(waves);
+  const auto pick = [&](auto is_bf16, auto stream_mode) {
+    return interleaved ? rows_kernel<MODE, is_bf16.value, true, stream_mode.value> : rows_kernel<MODE, is_bf16.value, false, stream_mode.value>;
+  };
+  const auto pick_stream = [&](auto is_bf16) {
+    return bytes >= kStreamAll ? pick(is_bf16, std::integral_constant<int, 2>())
+                               : bytes >= kStreamIn ? pick(is_bf16, std::integral_constant<int, 1>()) : pick(is_bf16, std::integral_constant<int, 0>());
+  };
+  const auto kernel = bf16 || MODE == kMove ? pick_stream(std::true_type()) : pick_stream(std::bool_constant<MODE == kMove>());
+  // (moves of more than the cache are done sooner in workgroups of one wave: 131072 rows of 8 heads 182 us, in ones of four 192 to 197;
+  // smaller ones, and the other calls, 0 to 4 % sooner in fours)
+  const uint32_t block_waves = MODE == kMove && bytes >= kStreamAll ? 1 : kRowThreads / 64;
+  // wave numbers stay below 2^25, and below 2^32 / waves for their quotient
+  int64_t most = (1 << 25) / waves;
+  if (most > ((int64_t)1 << 32) / waves / waves - 1) most = ((int64_t)1 << 32) / waves / waves - 1;
+  const int64_t groups = ((int64_t)n + (1 << a.group_log2) - 1) >> a.group_log2;
+  for (int64_t done = 0; done < groups; done += most) {
+    const int64_t m = groups - done < most ? groups - done : most;
+    a.first = done << a.group_log2;
+    a.end = (done + m) << a.group_log2 < n ? (done + m) << a.group_log2 : n;
+    a.n_waves = (uint32_t)(m * waves);
+    hipLaunchKernelGGL(kernel, dim3((a.n_waves + block_waves - 1) / block_waves), dim3(block_waves * 64), block_waves * 512 << a.group_log2, stream, a);
+  }
+  TL_HIP(hipGetLastError());
+  return TL_OK;
 }
 
 static tl_status check_rope(const char* who, const tl_rope* rope) {
@@ -341,41 +436,32 @@ static tl_status launch_rows(const char* who, const tl_rope* rope, const tl_qkv*
   if (rope && !pos_dev && (d->q || d->k)) TL_FAIL(TL_EINVAL, "%s: null positions", who);
   const int64_t size = d->is_bf16 ? 2 : 4;
   RowsArgs a{};
-  a.q = (const char*)d->q, a.k = (const char*)d->k, a.v = (const char*)d->v;
-  a.q_row = t[0].row * size, a.q_head = t[0].head * size;
-  a.k_row = t[1].row * size, a.k_head = t[1].head * size;
-  a.v_row = t[2].row * size, a.v_head = t[2].head * size;
-  a.q_out = (uint16_t*)d->q_out, a.k_out = (uint16_t*)d->k_out, a.v_out = (uint16_t*)d->v_out;
-  a.q_weight = d->q_weight, a.k_weight = d->k_weight;
+  int32_t heads[3];
+  for (int i = 0; i < 3; ++i) {
+    a.in[i] = (const char*)t[i].in;
+    a.row[i] = t[i].row * size;
+    a.head[i] = t[i].head * size;
+    a.out[i] = (uint16_t*)t[i].out;
+    heads[i] = t[i].in ? t[i].heads : 0;
+  }
+  a.weight[kQ] = d->q ? d->q_weight : nullptr;
+  a.weight[kK] = d->k ? d->k_weight : nullptr;
   a.eps = d->eps;
   a.pos = pos_dev;
   if (rope) {
     a.steps = rope->steps_dev;
     a.factor = rope->factor;
     a.rot_lanes = rope->rot_dim / 16;
-    a.interleaved = rope->interleaved != 0;
   }
-  a.q_heads = d->q ? d->q_heads : 0;
-  a.k_heads = d->k ? d->kv_heads : 0;
-  a.heads = a.q_heads + a.k_heads + (d->v ? d->kv_heads : 0);
-  if (pool) {
-    a.pool_k = (uint16_t*)pool->k_dev, a.pool_v = (uint16_t*)pool->v_dev;
-    a.pool_rows = pool_rows_dev;
-    a.n_pool_rows = pool->n_slots * pool->seg_len;
-  }
-  a.wave_blocks = (uint32_t)(a.heads + kWaveHeads - 1) / kWaveHeads;
-  const uint32_t most = launch_tokens(a.wave_blocks);
-  for (uint32_t first = 0; first < (uint32_t)n; first += most) {
-    const uint32_t m = (uint32_t)n - first < most ? (uint32_t)n - first : most;
-    a.first = first;
-    a.n_waves = m * a.wave_blocks;
-    const dim3 grid((a.n_waves + kRowThreads / 64 - 1) / (kRowThreads / 64)), block(kRowThreads);
-    const auto kernel = d->is_bf16 ? (pool ? rotate_rows_kernel<true, true> : rotate_rows_kernel<true, false>)
-                                   : (pool ? rotate_rows_kernel<false, true> : rotate_rows_kernel<false, false>);
-    hipLaunchKernelGGL(kernel, grid, block, 0, (hipStream_t)stream, a);
-  }
-  TL_HIP(hipGetLastError());
-  return TL_OK;
+  const bool interleaved = rope && rope->interleaved;
+  int64_t head_bytes = 0;
+  for (int i = 0; i < 3; ++i) head_bytes += heads[i] * (size + (t[i].out ? 2 : 0) + (pool && i != kQ ? 2 : 0)) * kHeadDim;
+  const int64_t bytes = head_bytes * n;
+  if (!pool) return launch<kDense>(a, heads, n, d->is_bf16 != 0, interleaved, bytes, (hipStream_t)stream);
+  a.pool[kK] = (uint16_t*)pool->k_dev, a.pool[kV] = (uint16_t*)pool->v_dev;
+  a.dst = pool_rows_dev;
+  a.n_pool_rows = pool->n_slots * pool->seg_len;
+  return launch<kToPool>(a, heads, n, d->is_bf16 != 0, interleaved, bytes, (hipStream_t)stream);
 }
 
 }  // namespace tl
@@ -425,27 +511,19 @@ tl_status tl_pool_move_rows(tl_pool* pool, const tl_rope* rope, const int32_t* s
   const tl_status st = check_rope("tl_pool_move_rows", rope);
   if (st != TL_OK) return st;
   if (!src_rows_dev || !dst_rows_dev || (rope && !shift_dev)) TL_FAIL(TL_EINVAL, "tl_pool_move_rows: null rows or shifts");
-  MoveArgs a{};
-  a.pool_k = (uint16_t*)pool->k_dev, a.pool_v = (uint16_t*)pool->v_dev;
-  a.src = src_rows_dev, a.dst = dst_rows_dev, a.shift = shift_dev;
+  RowsArgs a{};
+  const int32_t heads[3] = {0, pool->kv_heads, pool->kv_heads};
+  a.in[kK] = (const char*)pool->k_dev, a.in[kV] = (const char*)pool->v_dev;
+  a.pool[kK] = (uint16_t*)pool->k_dev, a.pool[kV] = (uint16_t*)pool->v_dev;
+  for (int i = kK; i <= kV; ++i) a.head[i] = kHeadDim * 2, a.row[i] = pool->kv_heads * a.head[i];
+  a.src = src_rows_dev, a.dst = dst_rows_dev, a.pos = shift_dev;
   if (rope) {
     a.steps = rope->steps_dev;
+    a.factor = 1.f;
     a.rot_lanes = rope->rot_dim / 16;
-    a.interleaved = rope->interleaved != 0;
   }
   a.n_pool_rows = pool->n_slots * pool->seg_len;
-  a.kv_heads = pool->kv_heads;
-  a.wave_blocks = (uint32_t)(2 * a.kv_heads + kWaveHeads - 1) / kWaveHeads;
-  const uint32_t most = launch_tokens(a.wave_blocks);
-  for (uint32_t first = 0; first < (uint32_t)n_rows; first += most) {
-    const uint32_t m = (uint32_t)n_rows - first < most ? (uint32_t)n_rows - first : most;
-    a.first = first;
-    a.n_waves = m * a.wave_blocks;
-    hipLaunchKernelGGL(move_rows_kernel, dim3((a.n_waves + kRowThreads / 64 - 1) / (kRowThreads / 64)), dim3(kRowThreads), 0,
-                       (hipStream_t)stream, a);
-  }
-  TL_HIP(hipGetLastError());
-  return TL_OK;
+  return launch<kMove>(a, heads, n_rows, true, rope && rope->interleaved, (int64_t)n_rows * pool->kv_heads * (8 * kHeadDim), (hipStream_t)stream);
 }
 
 }  // extern "C"

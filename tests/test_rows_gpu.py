@@ -231,6 +231,31 @@ def test_rotate_rows_offsets_beyond_32_bits():
     assert torch.equal(few, again)
 
 
+@pytest.mark.parametrize("mb,kind,norm", [(90, "bf16", True), (110, "bf16", True), (260, "bf16", True), (290, "fp32", False), (280, "bf16", False)])
+def test_rows_of_large_calls_are_the_rows_of_small_ones(mb, kind, norm):
+    """Calls on either side of what the cache behind HBM holds, whole and in place, to the bits of calls of a few hundred tokens."""
+    _say("%d MB" % mb)
+    q_heads, kv_heads = 9, 3
+    n = mb * 1000000 // ((q_heads + 2 * kv_heads) * 128 * (4 if kind == "bf16" else 6))
+    g = torch.Generator(device=DEV).manual_seed(mb)
+    x = torch.randn(n, q_heads + 2 * kv_heads, 128, generator=g, device=DEV).to(KIND[kind])
+    q, k, v = x[:, :q_heads], x[:, q_heads:q_heads + kv_heads], x[:, q_heads + kv_heads:]
+    pos = torch.randint(0, 1 << 20, (n,), generator=g, device=DEV, dtype=torch.int32)
+    qw, kw = _weights(mb) if norm else (None, None)
+    rope = _rope(_freqs(128))
+    outs = [torch.empty((n, h, 128), dtype=torch.bfloat16, device=DEV) for h in (q_heads, kv_heads, kv_heads)]
+    B.tl_rotate_rows(rope, pos, q, k, v, *outs, qw, kw)
+    for first in (0, 1000, n // 2 + 1, n - 333):
+        part = slice(first, first + 333)
+        few = [torch.empty((333, h, 128), dtype=torch.bfloat16, device=DEV) for h in (q_heads, kv_heads, kv_heads)]
+        B.tl_rotate_rows(rope, pos[part], q[part], k[part], v[part], *few, qw, kw)
+        assert all(torch.equal(a[part], b) for a, b in zip(outs, few))
+    if kind == "bf16":
+        again = [t.contiguous() for t in (q, k, v)]
+        B.tl_rotate_rows(rope, pos, *again, *again, qw, kw)
+        assert all(torch.equal(a, b) for a, b in zip(outs, again))
+
+
 # ---- the pool -----------------------------------------------------------------------------
 def _pool(n_slots, seg_len, kv_heads, seed=11):
     k, v = _randn(seed, n_slots, seg_len, kv_heads, 128), _randn(seed + 1, n_slots, seg_len, kv_heads, 128)
@@ -347,6 +372,34 @@ def test_move_rows_turns_keys_and_copies_values(n, kv_heads, rot, interleaved):
     B.tl_pool_move_rows(pool, _rope(freqs), bad, to, torch.ones_like(bad))
     B.tl_pool_move_rows(pool, _rope(freqs), bad[:0], to[:0], bad[:0])
     assert torch.equal(pk, k0)
+    B.tl_pool_destroy(pool)
+
+
+@pytest.mark.parametrize("kv_heads,seg_len,n", [(8, 64, 20000), (8, 256, 33001), (2, 512, 140001)])
+def test_moves_of_many_rows_are_moves_of_a_few(kv_heads, seg_len, n):
+    """The same on either side of the cache's size; rows of a large move in the order of the slots and scattered."""
+    _say("move %d rows" % n)
+    n_slots = 2 * n // seg_len + 2
+    g = torch.Generator(device=DEV).manual_seed(n)
+    pk, pv = (torch.randn(n_slots, seg_len, kv_heads, 128, generator=g, device=DEV).bfloat16() for _ in "kv")
+    k0, v0 = pk.clone(), pv.clone()
+    pool = B.tl_pool_create(n_slots, seg_len, kv_heads, 128, pk, pv)
+    order = torch.randperm(n_slots * seg_len, generator=g, device=DEV).to(torch.int32)
+    src, dst = order[:n].contiguous(), order[n:2 * n].sort().values
+    shift = torch.randint(-5000, 5000, (n,), generator=g, device=DEV, dtype=torch.int32)
+    rope = _rope(_freqs(128))
+    B.tl_pool_move_rows(pool, rope, src, dst, shift)
+    big_k, big_v = pk.clone(), pv.clone()
+    pk.copy_(k0), pv.copy_(v0)
+    for first in range(0, n, n // 3 + 1):
+        part = slice(first, min(n, first + n // 3 + 1))
+        B.tl_pool_move_rows(pool, rope, src[part], dst[part], shift[part])
+    assert torch.equal(pk, big_k) and torch.equal(pv, big_v)
+    at = torch.tensor([0, 1, n // 2, n - 1], device=DEV)
+    flat = pk.view(-1, kv_heads, 128)
+    want, tol = ro.rows(_np(k0.view(-1, kv_heads, 128)[src[at].long()]), shift[at].cpu().numpy(), _freqs(128))
+    _check(flat[dst[at].long()], want, tol, "keys")
+    assert torch.equal(pv.view(-1, kv_heads, 128)[dst.long()], v0.view(-1, kv_heads, 128)[src.long()])
     B.tl_pool_destroy(pool)
 
 

@@ -166,6 +166,11 @@ def test_other_arguments_that_are_refused():
     B.tl_pool_destroy(pool)
 
 
+def test_rows_are_packed_as_the_structure_is_laid_out():
+    args = (1, 2, 3, 4, -5, 6, 7, -8, 9, 10, 11, True, 0.5, 12, 13, 14, 15, 16)
+    assert B._PACK_QKV(*args) == bytes(B.tl_qkv(*args))
+
+
 def test_no_tokens_are_no_work():
     lib = B.load_library()
     assert lib.tl_rotate_rows(None, None, None, 0, None) == B.TL_OK
