@@ -442,14 +442,14 @@ def tl_rope_steps(inv_freq) -> np.ndarray:
 
 def tl_rope_of(steps, interleaved: bool = False, factor: float = 1.0) -> tl_rope:
     """steps: int64 device tensor [rot_dim / 2] with the bits of tl_rope_steps; the struct keeps it alive."""
-    _row_kinds()
-    at, n = _vector(steps, "steps", "i64", None, None)
-    rope = tl_rope(at, 2 * n, int(bool(interleaved)), factor)
-    rope.steps, rope.device, rope.at = steps, steps.get_device(), C.addressof(rope)
+    device = max(steps.get_device(), 0)
+    rope = tl_rope(_vector(steps, "steps", _row_kinds()["i64"], (len(steps),), device), 2 * len(steps), int(bool(interleaved)), factor)
+    rope.steps, rope.device, rope.at = steps, device, C.addressof(rope)
     return rope
 
 
 _ROW_KINDS = {}
+_MOST_ROWS = (1 << 31) - 1      # the C side counts in 32 bits, and ctypes would cut a larger number to them
 
 
 def _row_kinds():
@@ -460,74 +460,84 @@ def _row_kinds():
     return _ROW_KINDS
 
 
-def _vector(t, name, kind, n, device):
-    """(address, elements) of a dense one-dimensional device tensor of n elements (n None: any number)."""
-    if t.dtype is not _ROW_KINDS[kind]:
+def _vector(t, name, kind, shape, device):
+    """Address of a dense one-dimensional device tensor of the given shape."""
+    if t.dtype is not kind:
         raise TypeError("%s must be %s, is %s" % (name, kind, t.dtype))
-    dev, shape = t.get_device(), t.shape
-    if dev < 0 or (device is not None and dev != device):
+    if t.get_device() != device:
         raise ValueError("%s is on another device" % name)
-    if len(shape) != 1 or (n is not None and shape[0] != n) or not t.is_contiguous():
-        raise ValueError("%s must be dense [%s], is %s with strides %s" % (name, "n" if n is None else n, tuple(shape), t.stride()))
-    return t.data_ptr(), shape[0]
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be dense %s, is %s with strides %s" % (name, shape, tuple(t.shape), t.stride()))
+    return t.data_ptr()
 
 
 # tl_qkv as bytes: filling the ctypes structure field by field takes 0.8 us, this 0.2
 _PACK_QKV = Struct("3Q6q3if5Q").pack
 
 
+def _rows_of(x, name, dtype, n, device):
+    """(address, stride between tokens, between heads, shape) of [n, heads, 128]; the values of a head follow each other."""
+    if x.dtype is not dtype:
+        raise TypeError("%s must be %s, is %s" % (name, dtype, x.dtype))
+    if x.get_device() != device:
+        raise ValueError("%s is on another device" % name)
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 3 or shape[2] != 128 or stride[2] != 1 or shape[0] != n:
+        raise ValueError("%s must be [%d, heads, 128] with adjacent values, is %s with strides %s" % (name, n, tuple(shape), stride))
+    return x.data_ptr(), stride[0], stride[1], shape
+
+
+def _dense_of(x, name, shape, bf16, device):
+    if x.dtype is not bf16:
+        raise TypeError("%s must be bf16, is %s" % (name, x.dtype))
+    if x.get_device() != device:
+        raise ValueError("%s is on another device" % name)
+    if x.shape != shape or not x.is_contiguous():
+        raise ValueError("%s must be dense %s, is %s with strides %s" % (name, tuple(shape), tuple(x.shape), x.stride()))
+    return x.data_ptr()
+
+
 def _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps):
     """(tl_qkv's bytes, positions, tokens, device) of a call: shapes, types, strides and devices of its tensors are checked here."""
-    # (a decoded token's call takes as long here as in the launch: tensors are asked once for what is looked at)
+    # (a decoded token's call takes as long here as in the launch: tensors are asked for what is looked at, once)
     kinds = _ROW_KINDS or _row_kinds()
     some = q if q is not None else k if k is not None else v
     if some is None:
         raise ValueError("no rows")
-    dtype, device, bf16 = some.dtype, some.get_device(), kinds["bf16"]
+    dtype, device, n, bf16, f32 = some.dtype, some.get_device(), len(some), kinds["bf16"], kinds["f32"]
     if device < 0 or device != kinds["current"]():
         raise ValueError("rows must be on the current device")
-    if dtype is not bf16 and dtype is not kinds["f32"]:
+    if dtype is not bf16 and dtype is not f32:
         raise TypeError("rows must be bf16 or f32, are %s" % dtype)
-    n = len(some)
-    at, strides, heads, outs = [], [], [], []
-    for name, x, out in (("q", q, q_out), ("k", k, k_out), ("v", v, v_out)):
-        if x is None:
-            at.append(0)
-            strides += (0, 0)
-            heads.append(0)
-            outs.append(0 if out is None else out.data_ptr())         # (refused by the library)
-            continue
-        shape, stride = x.shape, x.stride()
-        if x.dtype is not dtype:
-            raise TypeError("%s must be %s, is %s" % (name, dtype, x.dtype))
-        if x.get_device() != device:
-            raise ValueError("%s is on another device" % name)
-        if len(shape) != 3 or shape[2] != 128 or stride[2] != 1 or shape[0] != n:
-            raise ValueError("%s must be [%d, heads, 128] with adjacent values, is %s with strides %s" % (name, n, tuple(shape), stride))
-        at.append(x.data_ptr())
-        strides += stride[:2]
-        heads.append(shape[1])
-        if out is None:
-            outs.append(0)
-            continue
-        if out.dtype is not bf16:
-            raise TypeError("%s_out must be bf16, is %s" % (name, out.dtype))
-        if out.get_device() != device:
-            raise ValueError("%s_out is on another device" % name)
-        if out.shape != shape or not out.is_contiguous():
-            raise ValueError("%s_out must be dense %s, is %s with strides %s" % (name, tuple(shape), tuple(out.shape), out.stride()))
-        outs.append(out.data_ptr())
-    if k is not None and v is not None and heads[1] != heads[2]:
-        raise ValueError("k has %d heads, v %d" % (heads[1], heads[2]))
-    qw = 0 if q_weight is None else _vector(q_weight, "q_weight", "f32", 128, device)[0]
-    kw = 0 if k_weight is None else _vector(k_weight, "k_weight", "f32", 128, device)[0]
-    where = None
+    if n > _MOST_ROWS:
+        raise ValueError("%d tokens in one call" % n)
+    qp = kp = vp = qr = qh = kr = kh = vr = vh = qo = ko = vo = qw = kw = 0
+    qs = ks = vs = (0, 0)
+    if q is not None:
+        qp, qr, qh, qs = _rows_of(q, "q", dtype, n, device)
+    if k is not None:
+        kp, kr, kh, ks = _rows_of(k, "k", dtype, n, device)
+    if v is not None:
+        vp, vr, vh, vs = _rows_of(v, "v", dtype, n, device)
+        if k is not None and vs != ks:
+            raise ValueError("k has %d heads, v %d" % (ks[1], vs[1]))
+    if q_out is not None:
+        qo = _dense_of(q_out, "q_out", qs, bf16, device)
+    if k_out is not None:
+        ko = _dense_of(k_out, "k_out", ks, bf16, device)
+    if v_out is not None:
+        vo = _dense_of(v_out, "v_out", vs, bf16, device)
+    if q_weight is not None:
+        qw = _vector(q_weight, "q_weight", f32, (128,), device)
+    if k_weight is not None:
+        kw = _vector(k_weight, "k_weight", f32, (128,), device)
+    at = None
     if rope is not None:
         if rope.device != device:
             raise ValueError("the rotation's steps are on another device")
         if pos is not None:
-            where = _vector(pos, "pos", "i32", n, device)[0]
-    return _PACK_QKV(*at, *strides, heads[0], heads[1] or heads[2], dtype is bf16, eps, qw, kw, *outs), where, n, device
+            at = _vector(pos, "pos", kinds["i32"], (n,), device)
+    return _PACK_QKV(qp, kp, vp, qr, qh, kr, kh, vr, vh, qs[1], ks[1] or vs[1], dtype is bf16, eps, qw, kw, qo, ko, vo), at, n, device
 
 
 def tl_rotate_rows(rope: Optional[tl_rope], pos, q=None, k=None, v=None, q_out=None, k_out=None, v_out=None, q_weight=None, k_weight=None,
@@ -542,25 +552,26 @@ def tl_pool_write_rows(pool: int, rope: Optional[tl_rope], pos, pool_rows, k, v,
                        k_weight=None, eps: float = 1e-6, stream=None):
     """tl_rotate_rows that writes k and v to the pool: token i's to pool row pool_rows[i] (int32 [n], -1: nowhere)."""
     rows, at, n, device = _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps)
-    _check(load_library().tl_pool_write_rows(pool, rope and rope.at, rows, at, _vector(pool_rows, "pool_rows", "i32", n, device)[0], n,
+    _check(load_library().tl_pool_write_rows(pool, rope and rope.at, rows, at, _vector(pool_rows, "pool_rows", _ROW_KINDS["i32"], (n,), device), n,
                                              _stream(stream)))
 
 
 def tl_pool_move_rows(pool: int, rope: Optional[tl_rope], src_rows, dst_rows, shift=None, stream=None):
     """Pool row src_rows[i] to dst_rows[i], keys turned on by shift[i] positions (int32 [n] each)."""
     kinds = _ROW_KINDS or _row_kinds()
-    src, n = _vector(src_rows, "src_rows", "i32", None, None)
-    device = src_rows.get_device()
-    if device != kinds["current"]():
+    i32, shape, device = kinds["i32"], (len(src_rows),), src_rows.get_device()
+    if device < 0 or device != kinds["current"]():
         raise ValueError("rows must be on the current device")
-    dst = _vector(dst_rows, "dst_rows", "i32", n, device)[0]
+    if shape[0] > _MOST_ROWS:
+        raise ValueError("%d rows in one call" % shape)
+    src, dst = _vector(src_rows, "src_rows", i32, shape, device), _vector(dst_rows, "dst_rows", i32, shape, device)
     at = None
     if rope is not None:
         if rope.device != device:
             raise ValueError("the rotation's steps are on another device")
         if shift is not None:
-            at = _vector(shift, "shift", "i32", n, device)[0]
-    _check(load_library().tl_pool_move_rows(pool, rope and rope.at, src, dst, at, n, _stream(stream)))
+            at = _vector(shift, "shift", i32, shape, device)
+    _check(load_library().tl_pool_move_rows(pool, rope and rope.at, src, dst, at, shape[0], _stream(stream)))
 
 
 def tl_set_option(knob: str, value: int):

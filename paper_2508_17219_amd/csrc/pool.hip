@@ -170,7 +170,7 @@ static int32_t take_slot(tl_pool* p, int32_t want) {
 }
 
 static void occupy(tl_pool* p, int32_t slot, uint64_t id, int32_t fill) {
-  p->slot_of.emplace(id, slot);
+  p->slot_of[id] = slot;
   p->id_of[slot] = id;
   p->fill[slot] = fill;
   p->refcnt[slot] = 1;
@@ -252,8 +252,17 @@ static tl_status place_rows(const char* who, tl_pool* pool, int32_t n_chains, co
     TL_FAIL(TL_EFULL, "%s: %d free slots, %d needed", who, pool->n_slots - pool->n_used, n_new_all);
   if (n_rows_all == 0) return TL_OK;
 
-  // ---- place the rows (host state changes from here on; no failure path below but HIP's) ----
+  // ---- memory for all that is about to be entered, or nothing is ----
   chunks.reserve((size_t)n_chains + n_new_all);
+  int32_t entered = 0;
+  try {
+    for (; entered < n_new_all; ++entered) pool->slot_of.emplace(new_ids[entered], -1);
+  } catch (...) {
+    while (entered > 0) pool->slot_of.erase(new_ids[--entered]);
+    throw;
+  }
+
+  // ---- place the rows (host state changes from here on; no failure path below but HIP's) ----
   for (int32_t c = 0; c < n_chains; ++c) {
     const int32_t n_rows = row_ptr[c + 1] - row_ptr[c];
     int32_t row = 0;
@@ -302,7 +311,11 @@ tl_status tl_pool_append_batch(tl_pool* pool, int32_t n_chains, const int32_t* h
   const int32_t C = pool->seg_len;
   hipStream_t st = (hipStream_t)stream;
   std::vector<AppendChunk> chunks;
-  rc = place_rows("tl_pool_append", pool, n_chains, has_tail, tail_ids, new_ptr, new_ids, row_ptr, new_slots_out, chunks);
+  try {
+    rc = place_rows("tl_pool_append", pool, n_chains, has_tail, tail_ids, new_ptr, new_ids, row_ptr, new_slots_out, chunks);
+  } catch (const std::bad_alloc&) {
+    TL_FAIL(TL_ENOMEM, "tl_pool_append: host allocation failed");
+  }
   if (rc != TL_OK || chunks.empty()) return rc;
   const size_t row16 = (size_t)pool->kv_heads * pool->head_dim * 2 / 16;
   const size_t slot16 = row16 * C;

@@ -401,6 +401,7 @@ static tl_status check_rows(const char* who, const tl_qkv* d, int64_t n, const t
     const __int128 rows = (__int128)(n - 1) * x.row * size, heads = (__int128)(x.heads - 1) * x.head * size;
     const __int128 base = (__int128)(uintptr_t)x.in;
     in[i] = {base + (rows < 0 ? rows : 0) + (heads < 0 ? heads : 0), base + (rows > 0 ? rows : 0) + (heads > 0 ? heads : 0) + kHeadDim * size};
+    if (in[i].lo < 0 || in[i].hi > (__int128)1 << 57) TL_FAIL(TL_EINVAL, "%s: strides of %s lead out of the address space", who, x.name);
   }
   for (int i = 0; i < 3; ++i) {
     if (!t[i].out) continue;

@@ -194,13 +194,12 @@ def test_rotate_rows_values_out_of_the_ordinary():
     vo = _out(8, 3)
     B.tl_rotate_rows(None, None, v=v, v_out=vo)
     assert torch.equal(vo.view(torch.int16), bits)
-    # every 32-bit value of a sweep is rounded to the nearest, ties to even, like torch does
-    sweep = torch.arange(0, 8 * 3 * 128, device=DEV, dtype=torch.int32).view(8, 3, 128) * 345679
-    f = sweep.view(torch.float32)
-    f = torch.where(torch.isfinite(f), f, torch.zeros_like(f))
-    B.tl_rotate_rows(None, None, v=f, v_out=vo)
-    normal = (f.abs() >= 1.2e-38) | (f == 0)                  # numbers below the normal ones may be flushed
-    assert torch.equal(vo[normal], f.to(torch.bfloat16)[normal])
+    # 32-bit values all over the range, those below the normal numbers too, are rounded to the nearest, ties to even, like torch does
+    for step in (345679, 2731):
+        f = (torch.arange(0, 8 * 3 * 128, device=DEV, dtype=torch.int32).view(8, 3, 128) * step).view(torch.float32)
+        f = torch.where(torch.isfinite(f), f, torch.zeros_like(f))
+        B.tl_rotate_rows(None, None, v=f, v_out=vo)
+        assert torch.equal(vo, f.to(torch.bfloat16))
 
 
 def test_rotate_rows_offsets_beyond_32_bits():

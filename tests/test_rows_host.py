@@ -134,7 +134,8 @@ def test_rotations_that_are_refused(rope, what):
     (dict(q_heads=0), "heads of q"), (dict(q_heads=-4), "heads of q"), (dict(q_heads=1 << 20), "heads of q"), (dict(kv_heads=0), "heads of k"),
     (dict(q_weight=0x5000, eps=0.0), "eps"), (dict(k_weight=0x5000, eps=-1.0), "eps"), (dict(q_weight=0x5000, eps=float("nan")), "eps"),
     (dict(q_weight=0x5000, eps=float("inf")), "eps"), (dict(q_weight=0x5000, eps=1e-40), "eps"),
-    (dict(q_row_stride=1 << 62), "strides of q"), (dict(v_head_stride=-(1 << 62)), "strides of v"),
+    (dict(q_row_stride=1 << 62), "strides of q"), (dict(k_row_stride=1 << 58), "strides of k"), (dict(v_row_stride=-(1 << 30)), "strides of v"),
+    (dict(q_head_stride=1 << 55), "strides of q"), (dict(v_head_stride=-(1 << 62)), "strides of v"),
     # an output over another input, over part of its own, over another output, over its own with other strides or of 32 bits
     (dict(k_out=0x100000 + 512), "overlaps q"), (dict(q_out=0x100000 + 256), "overlaps q"), (dict(k_out=0x600000 + 1024), "outputs of k and v overlap"),
     (dict(q_out=0x100000, q_row_stride=640), "overlaps q"), (dict(q_out=0x100000, is_bf16=0), "overlaps q"),
