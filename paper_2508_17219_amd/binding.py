@@ -504,7 +504,7 @@ def _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps):
     some = q if q is not None else k if k is not None else v
     if some is None:
         raise ValueError("no rows")
-    dtype, device, n, bf16, f32 = some.dtype, some.get_device(), len(some), kinds["bf16"], kinds["f32"]
+    dtype, device, n, bf16, f32 = some.dtype, some.get_device(), some.shape[0], kinds["bf16"], kinds["f32"]
     if device < 0 or device != kinds["current"]():
         raise ValueError("rows must be on the current device")
     if dtype is not bf16 and dtype is not f32:
@@ -559,11 +559,12 @@ def tl_pool_write_rows(pool: int, rope: Optional[tl_rope], pos, pool_rows, k, v,
 def tl_pool_move_rows(pool: int, rope: Optional[tl_rope], src_rows, dst_rows, shift=None, stream=None):
     """Pool row src_rows[i] to dst_rows[i], keys turned on by shift[i] positions (int32 [n] each)."""
     kinds = _ROW_KINDS or _row_kinds()
-    i32, shape, device = kinds["i32"], (len(src_rows),), src_rows.get_device()
+    i32, n, device = kinds["i32"], src_rows.numel(), src_rows.get_device()
     if device < 0 or device != kinds["current"]():
         raise ValueError("rows must be on the current device")
-    if shape[0] > _MOST_ROWS:
-        raise ValueError("%d rows in one call" % shape)
+    if n > _MOST_ROWS:
+        raise ValueError("%d rows in one call" % n)
+    shape = (n,)
     src, dst = _vector(src_rows, "src_rows", i32, shape, device), _vector(dst_rows, "dst_rows", i32, shape, device)
     at = None
     if rope is not None:
@@ -571,7 +572,7 @@ def tl_pool_move_rows(pool: int, rope: Optional[tl_rope], src_rows, dst_rows, sh
             raise ValueError("the rotation's steps are on another device")
         if shift is not None:
             at = _vector(shift, "shift", i32, shape, device)
-    _check(load_library().tl_pool_move_rows(pool, rope and rope.at, src, dst, at, shape[0], _stream(stream)))
+    _check(load_library().tl_pool_move_rows(pool, rope and rope.at, src, dst, at, n, _stream(stream)))
 
 
 def tl_set_option(knob: str, value: int):

@@ -487,8 +487,12 @@ def test_binding_refuses_shapes_and_kinds():
         B.tl_pool_write_rows(pool, rope, pos, pos, q, q)             # 4 heads into a pool of 2
     with pytest.raises(ValueError):
         B.tl_pool_write_rows(pool, rope, pos, pos[:2], k, k)
-    with pytest.raises(ValueError):
-        B.tl_pool_move_rows(pool, rope, pos, pos[:2], pos)
+    for bad in ((pos, pos[:2], pos), (pos[:2], pos, pos), (pos, pos, pos[:2]), (pos.view(2, 2), pos, pos), (pos.view(2, 2), pos.view(2, 2), pos.view(2, 2)),
+                (pos, pos.cpu(), pos), (torch.arange(8, dtype=torch.int32, device=DEV)[::2], pos, pos)):
+        with pytest.raises(ValueError):
+            B.tl_pool_move_rows(pool, rope, *bad)
+    with pytest.raises(TypeError):
+        B.tl_pool_move_rows(pool, rope, pos, pos.long(), pos)
     with pytest.raises(B.TokenLakeError):
         B.tl_pool_move_rows(pool, rope, pos, pos)
     B.tl_pool_destroy(pool)
