@@ -444,7 +444,7 @@ def tl_rope_of(steps, interleaved: bool = False, factor: float = 1.0) -> tl_rope
     """steps: int64 device tensor [rot_dim / 2] with the bits of tl_rope_steps; the struct keeps it alive."""
     device = max(steps.get_device(), 0)
     rope = tl_rope(_vector(steps, "steps", _row_kinds()["i64"], (len(steps),), device), 2 * len(steps), int(bool(interleaved)), factor)
-    rope.steps, rope.device, rope.at = steps, device, C.addressof(rope)
+    rope.steps, rope.device = steps, device
     return rope
 
 
@@ -540,19 +540,23 @@ def _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps):
     return _PACK_QKV(qp, kp, vp, qr, qh, kr, kh, vr, vh, qs[1], ks[1] or vs[1], dtype is bf16, eps, qw, kw, qo, ko, vo), at, n, device
 
 
+def _at(rope) -> Optional[int]:
+    return None if rope is None else C.addressof(rope)
+
+
 def tl_rotate_rows(rope: Optional[tl_rope], pos, q=None, k=None, v=None, q_out=None, k_out=None, v_out=None, q_weight=None, k_weight=None,
                    eps: float = 1e-6, stream=None):
     """Norms (with weights) and rotation (with rope) of q [n, q_heads, 128] and k [n, kv_heads, 128] with any strides between tokens and
     heads, bf16 or fp32; v as it is; to dense bf16 tensors.  pos: int32 [n]."""
     rows, at, n, _ = _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps)
-    _check(load_library().tl_rotate_rows(rope and rope.at, rows, at, n, _stream(stream)))
+    _check(load_library().tl_rotate_rows(_at(rope), rows, at, n, _stream(stream)))
 
 
 def tl_pool_write_rows(pool: int, rope: Optional[tl_rope], pos, pool_rows, k, v, q=None, q_out=None, k_out=None, v_out=None, q_weight=None,
                        k_weight=None, eps: float = 1e-6, stream=None):
     """tl_rotate_rows that writes k and v to the pool: token i's to pool row pool_rows[i] (int32 [n], -1: nowhere)."""
     rows, at, n, device = _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps)
-    _check(load_library().tl_pool_write_rows(pool, rope and rope.at, rows, at, _vector(pool_rows, "pool_rows", _ROW_KINDS["i32"], (n,), device), n,
+    _check(load_library().tl_pool_write_rows(pool, _at(rope), rows, at, _vector(pool_rows, "pool_rows", _ROW_KINDS["i32"], (n,), device), n,
                                              _stream(stream)))
 
 
@@ -572,7 +576,7 @@ def tl_pool_move_rows(pool: int, rope: Optional[tl_rope], src_rows, dst_rows, sh
             raise ValueError("the rotation's steps are on another device")
         if shift is not None:
             at = _vector(shift, "shift", i32, shape, device)
-    _check(load_library().tl_pool_move_rows(pool, rope and rope.at, src, dst, at, n, _stream(stream)))
+    _check(load_library().tl_pool_move_rows(pool, _at(rope), src, dst, at, n, _stream(stream)))
 
 
 def tl_set_option(knob: str, value: int):
