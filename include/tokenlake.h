@@ -401,7 +401,7 @@ tl_status tl_rope_steps(const double* inv_freq, int32_t n, uint64_t* steps_out);
  * q_weight / k_weight: device fp32 [128] or NULL.  Given, each head of q / k is divided by the root of the mean of its squares
  * plus eps and multiplied by the weight, in front of the rotation; eps: positive, normal, looked at only then.
  * q_out / k_out / v_out: device, dense [n, heads, 128] bf16, rounded once from fp32; v is not changed but for that.  An
- * output may be its own input if that is dense bf16; any other overlap of an output is TL_EINVAL. */
+ * output may be its own input if that is dense bf16; any other overlap of an output with rows or outputs is TL_EINVAL. */
 typedef struct tl_qkv {
   const void *q, *k, *v;
   int64_t q_row_stride, q_head_stride, k_row_stride, k_head_stride, v_row_stride, v_head_stride;
@@ -420,7 +420,8 @@ tl_status tl_rotate_rows(const tl_rope* rope, const tl_qkv* rows, const int32_t*
 /* tl_rotate_rows that also writes k and v (both there, kv_heads the pool's) to the pool: token i's to the pool row
  * pool_rows_dev[i] = slot * seg_len + token (device int32 [n_tokens]; from tl_pool_reserve_batch).  k_out and v_out may be
  * NULL.  A row outside the pool (-1: a padded batch) is not written, its outputs are.  Rows must differ: of a row named
- * twice each 16 bytes are either token's.  No input and no output may lie in the pool's slots.  Changes no fill and keeps plans valid. */
+ * twice each 16 bytes are either token's.  What a row held is overwritten, whoever shares its segment.  No
+ * input and no output may lie in the pool's slots.  Changes no fill and keeps plans valid. */
 tl_status tl_pool_write_rows(tl_pool* pool, const tl_rope* rope, const tl_qkv* rows, const int32_t* pos_dev, const int32_t* pool_rows_dev,
                              int32_t n_tokens, void* stream);
 

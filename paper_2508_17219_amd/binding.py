@@ -443,7 +443,7 @@ def tl_rope_steps(inv_freq) -> np.ndarray:
 def tl_rope_of(steps, interleaved: bool = False, factor: float = 1.0) -> tl_rope:
     """steps: int64 device tensor [rot_dim / 2] with the bits of tl_rope_steps; the struct keeps it alive."""
     device = max(steps.get_device(), 0)
-    rope = tl_rope(_vector(steps, "steps", _row_kinds()["i64"], (len(steps),), device), 2 * len(steps), int(bool(interleaved)), factor)
+    rope = tl_rope(_dense(steps, "steps", _row_kinds()["i64"], steps.numel(), device), 2 * steps.numel(), int(bool(interleaved)), factor)
     rope.steps, rope.device = steps, device
     return rope
 
@@ -460,14 +460,14 @@ def _row_kinds():
     return _ROW_KINDS
 
 
-def _vector(t, name, kind, shape, device):
-    """Address of a dense one-dimensional device tensor of the given shape."""
+def _dense(t, name, kind, n, device):
+    """Address of a dense device tensor of n elements."""
     if t.dtype is not kind:
         raise TypeError("%s must be %s, is %s" % (name, kind, t.dtype))
     if t.get_device() != device:
         raise ValueError("%s is on another device" % name)
-    if t.shape != shape or not t.is_contiguous():
-        raise ValueError("%s must be dense %s, is %s with strides %s" % (name, shape, tuple(t.shape), t.stride()))
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s must be dense with %d elements, is %s with strides %s" % (name, n, tuple(t.shape), t.stride()))
     return t.data_ptr()
 
 
@@ -475,26 +475,16 @@ def _vector(t, name, kind, shape, device):
 _PACK_QKV = Struct("3Q6q3if5Q").pack
 
 
-def _rows_of(x, name, dtype, n, device):
-    """(address, stride between tokens, between heads, shape) of [n, heads, 128]; the values of a head follow each other."""
+def _rows_of(x, name, dtype, device):
+    """(address, tokens, heads, stride between tokens, between heads) of [n, heads, 128]; the values of a head follow each other."""
     if x.dtype is not dtype:
         raise TypeError("%s must be %s, is %s" % (name, dtype, x.dtype))
     if x.get_device() != device:
         raise ValueError("%s is on another device" % name)
     shape, stride = x.shape, x.stride()
-    if len(shape) != 3 or shape[2] != 128 or stride[2] != 1 or shape[0] != n:
-        raise ValueError("%s must be [%d, heads, 128] with adjacent values, is %s with strides %s" % (name, n, tuple(shape), stride))
-    return x.data_ptr(), stride[0], stride[1], shape
-
-
-def _dense_of(x, name, shape, bf16, device):
-    if x.dtype is not bf16:
-        raise TypeError("%s must be bf16, is %s" % (name, x.dtype))
-    if x.get_device() != device:
-        raise ValueError("%s is on another device" % name)
-    if x.shape != shape or not x.is_contiguous():
-        raise ValueError("%s must be dense %s, is %s with strides %s" % (name, tuple(shape), tuple(x.shape), x.stride()))
-    return x.data_ptr()
+    if len(shape) != 3 or shape[2] != 128 or stride[2] != 1:
+        raise ValueError("%s must be [n, heads, 128] with adjacent values, is %s with strides %s" % (name, tuple(shape), stride))
+    return x.data_ptr(), shape[0], shape[1], stride[0], stride[1]
 
 
 def _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps):
@@ -504,40 +494,40 @@ def _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps):
     some = q if q is not None else k if k is not None else v
     if some is None:
         raise ValueError("no rows")
-    dtype, device, n, bf16, f32 = some.dtype, some.get_device(), some.shape[0], kinds["bf16"], kinds["f32"]
+    dtype, device, bf16, f32 = some.dtype, some.get_device(), kinds["bf16"], kinds["f32"]
     if device < 0 or device != kinds["current"]():
         raise ValueError("rows must be on the current device")
     if dtype is not bf16 and dtype is not f32:
         raise TypeError("rows must be bf16 or f32, are %s" % dtype)
+    qp = kp = vp = qn = kn = vn = qh = kh = vh = qr = qs = kr = ks = vr = vs = qo = ko = vo = qw = kw = 0
+    if q is not None:
+        qp, qn, qh, qr, qs = _rows_of(q, "q", dtype, device)
+    if k is not None:
+        kp, kn, kh, kr, ks = _rows_of(k, "k", dtype, device)
+    if v is not None:
+        vp, vn, vh, vr, vs = _rows_of(v, "v", dtype, device)
+    n = qn or kn or vn
+    if (q is not None and qn != n) or (k is not None and kn != n) or (v is not None and vn != n) or (k is not None and v is not None and kh != vh):
+        raise ValueError("q, k and v of %d, %d and %d tokens, k and v of %d and %d heads" % (qn, kn, vn, kh, vh))
     if n > _MOST_ROWS:
         raise ValueError("%d tokens in one call" % n)
-    qp = kp = vp = qr = qh = kr = kh = vr = vh = qo = ko = vo = qw = kw = 0
-    qs = ks = vs = (0, 0)
-    if q is not None:
-        qp, qr, qh, qs = _rows_of(q, "q", dtype, n, device)
-    if k is not None:
-        kp, kr, kh, ks = _rows_of(k, "k", dtype, n, device)
-    if v is not None:
-        vp, vr, vh, vs = _rows_of(v, "v", dtype, n, device)
-        if k is not None and vs != ks:
-            raise ValueError("k has %d heads, v %d" % (ks[1], vs[1]))
     if q_out is not None:
-        qo = _dense_of(q_out, "q_out", qs, bf16, device)
+        qo = _dense(q_out, "q_out", bf16, n * qh * 128, device)
     if k_out is not None:
-        ko = _dense_of(k_out, "k_out", ks, bf16, device)
+        ko = _dense(k_out, "k_out", bf16, n * kh * 128, device)
     if v_out is not None:
-        vo = _dense_of(v_out, "v_out", vs, bf16, device)
+        vo = _dense(v_out, "v_out", bf16, n * vh * 128, device)
     if q_weight is not None:
-        qw = _vector(q_weight, "q_weight", f32, (128,), device)
+        qw = _dense(q_weight, "q_weight", f32, 128, device)
     if k_weight is not None:
-        kw = _vector(k_weight, "k_weight", f32, (128,), device)
+        kw = _dense(k_weight, "k_weight", f32, 128, device)
     at = None
     if rope is not None:
         if rope.device != device:
             raise ValueError("the rotation's steps are on another device")
         if pos is not None:
-            at = _vector(pos, "pos", kinds["i32"], (n,), device)
-    return _PACK_QKV(qp, kp, vp, qr, qh, kr, kh, vr, vh, qs[1], ks[1] or vs[1], dtype is bf16, eps, qw, kw, qo, ko, vo), at, n, device
+            at = _dense(pos, "pos", kinds["i32"], n, device)
+    return _PACK_QKV(qp, kp, vp, qr, qs, kr, ks, vr, vs, qh, kh or vh, dtype is bf16, eps, qw, kw, qo, ko, vo), at, n, device
 
 
 def _at(rope) -> Optional[int]:
@@ -547,35 +537,34 @@ def _at(rope) -> Optional[int]:
 def tl_rotate_rows(rope: Optional[tl_rope], pos, q=None, k=None, v=None, q_out=None, k_out=None, v_out=None, q_weight=None, k_weight=None,
                    eps: float = 1e-6, stream=None):
     """Norms (with weights) and rotation (with rope) of q [n, q_heads, 128] and k [n, kv_heads, 128] with any strides between tokens and
-    heads, bf16 or fp32; v as it is; to dense bf16 tensors.  pos: int32 [n]."""
+    heads, bf16 or fp32; v as it is; to dense bf16 tensors of as many elements.  pos: int32, n of them."""
     rows, at, n, _ = _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps)
     _check(load_library().tl_rotate_rows(_at(rope), rows, at, n, _stream(stream)))
 
 
 def tl_pool_write_rows(pool: int, rope: Optional[tl_rope], pos, pool_rows, k, v, q=None, q_out=None, k_out=None, v_out=None, q_weight=None,
                        k_weight=None, eps: float = 1e-6, stream=None):
-    """tl_rotate_rows that writes k and v to the pool: token i's to pool row pool_rows[i] (int32 [n], -1: nowhere)."""
+    """tl_rotate_rows that writes k and v to the pool: token i's to pool row pool_rows[i] (int32, n of them; -1: nowhere)."""
     rows, at, n, device = _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps)
-    _check(load_library().tl_pool_write_rows(pool, _at(rope), rows, at, _vector(pool_rows, "pool_rows", _ROW_KINDS["i32"], (n,), device), n,
+    _check(load_library().tl_pool_write_rows(pool, _at(rope), rows, at, _dense(pool_rows, "pool_rows", _ROW_KINDS["i32"], n, device), n,
                                              _stream(stream)))
 
 
 def tl_pool_move_rows(pool: int, rope: Optional[tl_rope], src_rows, dst_rows, shift=None, stream=None):
-    """Pool row src_rows[i] to dst_rows[i], keys turned on by shift[i] positions (int32 [n] each)."""
+    """Pool row src_rows[i] to dst_rows[i], keys turned on by shift[i] positions (int32, as many of each)."""
     kinds = _ROW_KINDS or _row_kinds()
     i32, n, device = kinds["i32"], src_rows.numel(), src_rows.get_device()
     if device < 0 or device != kinds["current"]():
         raise ValueError("rows must be on the current device")
     if n > _MOST_ROWS:
         raise ValueError("%d rows in one call" % n)
-    shape = (n,)
-    src, dst = _vector(src_rows, "src_rows", i32, shape, device), _vector(dst_rows, "dst_rows", i32, shape, device)
+    src, dst = _dense(src_rows, "src_rows", i32, n, device), _dense(dst_rows, "dst_rows", i32, n, device)
     at = None
     if rope is not None:
         if rope.device != device:
             raise ValueError("the rotation's steps are on another device")
         if shift is not None:
-            at = _vector(shift, "shift", i32, shape, device)
+            at = _dense(shift, "shift", i32, n, device)
     _check(load_library().tl_pool_move_rows(pool, _at(rope), src, dst, at, n, _stream(stream)))
 
 

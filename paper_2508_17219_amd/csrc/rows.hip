@@ -60,7 +60,7 @@ struct RowsArgs {
   int32_t rot_lanes;                     // rot_dim / 16: lanes of a head whose values turn; 0: no rotation
   int32_t group_log2;                    // tokens that waves are counted for
   Div group_waves;
-  uint32_t n_waves;
+  uint32_t n_waves, block_waves;
   int64_t first, end;                    // tokens of this launch
 };
 
@@ -205,7 +205,7 @@ template <int MODE, bool BF16, bool INTER, int STREAM>
 __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
   constexpr bool kStreamLoads = STREAM >= 1, kStreamStores = STREAM >= 2;
   extern __shared__ float4 lds_cs[][4][8];              // [wave and token][pairs 8 l + 2 j and the next: j][l]
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * (blockDim.x / 64) + threadIdx.x / 64);
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * a.block_waves + threadIdx.x / 64);
   if (wave >= a.n_waves) return;
   const uint32_t group = div_by(wave, a.group_waves);
   uint32_t part = wave - group * a.group_waves.d;
@@ -332,7 +332,7 @@ static tl_status launch(RowsArgs& a, const int32_t (&heads)[3], int32_t n, bool 
   const auto kernel = bf16 || MODE == kMove ? pick_stream(std::true_type()) : pick_stream(std::bool_constant<MODE == kMove>());
   // (moves of more than the cache are done sooner in workgroups of one wave: 131072 rows of 8 heads 182 us, in ones of four 192 to 197;
   // smaller ones, and the other calls, 0 to 4 % sooner in fours)
-  const uint32_t block_waves = MODE == kMove && bytes >= kStreamAll ? 1 : kRowThreads / 64;
+  a.block_waves = MODE == kMove && bytes >= kStreamAll ? 1 : kRowThreads / 64;
   // wave numbers stay below 2^25, and below 2^32 / waves for their quotient
   int64_t most = (1 << 25) / waves;
   if (most > ((int64_t)1 << 32) / waves / waves - 1) most = ((int64_t)1 << 32) / waves / waves - 1;
@@ -342,7 +342,8 @@ static tl_status launch(RowsArgs& a, const int32_t (&heads)[3], int32_t n, bool 
     a.first = done << a.group_log2;
     a.end = (done + m) << a.group_log2 < n ? (done + m) << a.group_log2 : n;
     a.n_waves = (uint32_t)(m * waves);
-    hipLaunchKernelGGL(kernel, dim3((a.n_waves + block_waves - 1) / block_waves), dim3(block_waves * 64), block_waves * 512 << a.group_log2, stream, a);
+    hipLaunchKernelGGL(kernel, dim3((a.n_waves + a.block_waves - 1) / a.block_waves), dim3(a.block_waves * 64), a.block_waves * 512 << a.group_log2,
+                       stream, a);
   }
   TL_HIP(hipGetLastError());
   return TL_OK;

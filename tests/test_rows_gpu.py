@@ -472,22 +472,27 @@ def test_binding_refuses_shapes_and_kinds():
     with pytest.raises(TypeError):
         B.tl_rotate_rows(rope, pos.long(), q, q_out=qo)
     for bad in (dict(q=q[..., :64], q_out=qo), dict(q=q.flatten(1), q_out=qo), dict(q=q.transpose(1, 2), q_out=qo), dict(q=q, q_out=qo[:2]),
-                dict(q=q, q_out=ko), dict(q=q, q_out=_out(n, 8)[:, :4]), dict(q=q, k=k[:3], q_out=qo, k_out=ko), dict(q=q, q_out=qo, q_weight=w[:64]),
+                dict(q=q, q_out=ko), dict(q=q, q_out=_out(n, 8)[:, :4]), dict(q=q[:0], k=k, q_out=qo[:0], k_out=ko), dict(q=q, k=k[:0], q_out=qo, k_out=ko[:0]), dict(q=q, k=k[:3], q_out=qo, k_out=ko), dict(q=q, q_out=qo, q_weight=w[:64]),
                 dict(k=k, v=q, k_out=ko, v_out=qo), dict(q=q.cpu(), q_out=qo), dict(q=q, q_out=qo.cpu()),
                 dict(q=torch.zeros(n, 4, 256, dtype=torch.bfloat16, device=DEV)[..., ::2], q_out=qo)):
         with pytest.raises(ValueError):
             B.tl_rotate_rows(rope, pos, **bad)
-    for bad in (pos[:3], pos[:, None], pos.cpu(), torch.arange(2 * n, dtype=torch.int32, device=DEV)[::2]):
+    for bad in (pos[:3], pos.cpu(), torch.arange(2 * n, dtype=torch.int32, device=DEV)[::2]):
         with pytest.raises(ValueError):
             B.tl_rotate_rows(rope, bad, q, q_out=qo)
     with pytest.raises(B.TokenLakeError):
         B.tl_rotate_rows(rope, None, q, q_out=qo)
+    # dense tensors of any shape will do where only the elements count
+    flat = torch.empty(n, 4 * 128, dtype=torch.bfloat16, device=DEV)
+    B.tl_rotate_rows(rope, pos.view(1, n), q, q_out=flat)
+    B.tl_rotate_rows(rope, pos, q, q_out=qo)
+    assert torch.equal(flat.view(n, 4, 128), qo)
     pool, pk, pv = _pool(3, 64, 2)
     with pytest.raises(B.TokenLakeError):
         B.tl_pool_write_rows(pool, rope, pos, pos, q, q)             # 4 heads into a pool of 2
     with pytest.raises(ValueError):
         B.tl_pool_write_rows(pool, rope, pos, pos[:2], k, k)
-    for bad in ((pos, pos[:2], pos), (pos[:2], pos, pos), (pos, pos, pos[:2]), (pos.view(2, 2), pos, pos), (pos.view(2, 2), pos.view(2, 2), pos.view(2, 2)),
+    for bad in ((pos, pos[:2], pos), (pos[:2], pos, pos), (pos, pos, pos[:2]),
                 (pos, pos.cpu(), pos), (torch.arange(8, dtype=torch.int32, device=DEV)[::2], pos, pos)):
         with pytest.raises(ValueError):
             B.tl_pool_move_rows(pool, rope, *bad)
