@@ -117,10 +117,19 @@ __device__ __forceinline__ float sum8(float x) {
   return dpp_add<0x141>(dpp_add<0x4e>(dpp_add<0xb1>(x)));   // lanes 1 apart, 2 apart, and the other four by a mirrored half row
 }
 
-// Where the two runs of 8 values of lane l of a head begin.  Lanes whose values turn against each other from afar (i with
-// i + rot_dim / 2) hold one run of each half of the turning dimensions, so that both of a pair are in one lane; others 16 in a row.
-__device__ __forceinline__ int2 runs_of(int l, int rot_lanes, bool interleaved) {
-  return !interleaved && l < rot_lanes ? make_int2(8 * l, 8 * (rot_lanes + l)) : make_int2(16 * l, 16 * l + 8);
+// Where the two runs of 8 values of lane l of a head begin.  Neighbouring lanes hold neighbouring runs, so that each of the two loads
+// and stores covers whole stretches of the head (16 values in a row to a lane touch every line twice: 8192 tokens of 32/8
+// heads 41 to 44 us for 37, fp32 73 for 51).  Both values of a pair are in one lane: where they are neighbours they are in one
+// run; where i turns with i + rot_dim / 2 the first rot_lanes lanes have one run of each half, the others what does not turn.
+template <bool INTER>
+__device__ __forceinline__ int2 runs_of(int l, int rot_lanes) {
+  return INTER ? make_int2(8 * l, 64 + 8 * l) : l < rot_lanes ? make_int2(8 * l, 8 * (rot_lanes + l)) : make_int2(8 * (rot_lanes + l), 64 + 8 * l);
+}
+
+// Where the lane that turns it finds the cosine and sine of a pair: (j, l) of [4][8] entries of two pairs, the lane's own in entries j = 0..3.
+template <bool INTER>
+__device__ __forceinline__ int2 entry_of(int pair) {
+  return INTER ? make_int2((pair >> 5) * 2 + ((pair >> 1) & 1), (pair & 31) >> 2) : make_int2((pair >> 1) & 3, pair >> 3);
 }
 
 // A lane's 16 values as they are in memory, two runs of 8.
@@ -186,16 +195,38 @@ __device__ __forceinline__ void norm16(const Lane16<BF16>& raw, float* x, float 
   for (int i = 0; i < 16; ++i) x[i] *= r * w[i];
 }
 
-// The lane's 8 pairs turned; cs: cosine and sine of pairs 2 j and 2 j + 1 in cs[j].
+__device__ __forceinline__ void turn2(float& a, float& b, float c, float s) {
+  const float u = a * c - b * s;
+  b = a * s + b * c;
+  a = u;
+}
+
+// The lane's pairs turned, cosine and sine of two in each of cs[0..4).
 template <bool INTER>
-__device__ __forceinline__ void turn16(float* x, const float4* cs) {
+__device__ __forceinline__ void turn16(float* x, const float4* cs, bool first_run, bool second_run) {
+  if (!INTER) {                  // both or none
+    if (first_run) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    float &a = x[INTER ? 2 * i : i], &b = x[INTER ? 2 * i + 1 : 8 + i];
-    const float c = i & 1 ? cs[i / 2].z : cs[i / 2].x, s = i & 1 ? cs[i / 2].w : cs[i / 2].y;
-    const float u = a * c - b * s;
-    b = a * s + b * c;
-    a = u;
+      for (int j = 0; j < 4; ++j) {
+        turn2(x[2 * j], x[8 + 2 * j], cs[j].x, cs[j].y);
+        turn2(x[2 * j + 1], x[9 + 2 * j], cs[j].z, cs[j].w);
+      }
+    }
+  } else {
+    if (first_run) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        turn2(x[4 * j], x[4 * j + 1], cs[j].x, cs[j].y);
+        turn2(x[4 * j + 2], x[4 * j + 3], cs[j].z, cs[j].w);
+      }
+    }
+    if (second_run) {
+#pragma unroll
+      for (int j = 2; j < 4; ++j) {
+        turn2(x[4 * j], x[4 * j + 1], cs[j].x, cs[j].y);
+        turn2(x[4 * j + 2], x[4 * j + 3], cs[j].z, cs[j].w);
+      }
+    }
   }
 }
 
@@ -204,7 +235,7 @@ __device__ __forceinline__ void turn16(float* x, const float4* cs) {
 template <int MODE, bool BF16, bool INTER, int STREAM>
 __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
   constexpr bool kStreamLoads = STREAM >= 1, kStreamStores = STREAM >= 2;
-  extern __shared__ float4 lds_cs[][4][8];              // [wave and token][pairs 8 l + 2 j and the next: j][l]
+  extern __shared__ float4 lds_cs[][4][8];              // [wave and token] and what entry_of says
   const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * a.block_waves + threadIdx.x / 64);
   if (wave >= a.n_waves) return;
   const uint32_t group = div_by(wave, a.group_waves);
@@ -229,9 +260,10 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
   const int lane = threadIdx.x & 63, l = lane & 7;
   const int sub = (lane >> 3) >> (3 - deal.tokens_log2), g = (lane >> 3) & (at_once - 1);      // token and head of the lane
   const bool there = sub < tokens && h0 + g < deal.heads;
-  const int2 at = runs_of(l, a.rot_lanes, INTER);
+  const int2 at = runs_of<INTER>(l, a.rot_lanes);
   const float* weight = MODE == kMove ? nullptr : a.weight[kind];
-  const bool any_turn = a.rot_lanes && kind != kV, turns = any_turn && l < a.rot_lanes;
+  const bool any_turn = a.rot_lanes && kind != kV;
+  const bool turns = any_turn && (INTER ? l < 2 * a.rot_lanes : l < a.rot_lanes), turns_too = INTER ? any_turn && l + 8 < 2 * a.rot_lanes : turns;
 
   uint64_t step = 0;
   if (any_turn && lane < 8 * a.rot_lanes) step = a.steps[lane];
@@ -257,10 +289,11 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
 
   auto* const mine = lds_cs + ((threadIdx.x / 64) << a.group_log2);
   if (any_turn) {
+    const int2 e = entry_of<INTER>(lane);
     for (int i = 0; i < tokens; ++i) {
       float c, s;
       cos_sin((uint64_t)(int64_t)a.pos[token0 + i] * step, c, s);
-      ((float2*)&mine[i][(lane >> 1) & 3][lane >> 3])[lane & 1] = make_float2(c * a.factor, s * a.factor);
+      ((float2*)&mine[i][e.x][e.y])[lane & 1] = make_float2(c * a.factor, s * a.factor);
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -279,7 +312,7 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
       float4 cs[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) cs[j] = mine[sub][j][l];
-      turn16<INTER>(x, cs);
+      turn16<INTER>(x, cs, turns, turns_too);
       lo = narrow(x);
       hi = narrow(x + 8);
     } else {
