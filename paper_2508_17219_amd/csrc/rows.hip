@@ -117,19 +117,27 @@ __device__ __forceinline__ float sum8(float x) {
   return dpp_add<0x141>(dpp_add<0x4e>(dpp_add<0xb1>(x)));   // lanes 1 apart, 2 apart, and the other four by a mirrored half row
 }
 
-// Where the two runs of 8 values of lane l of a head begin.  Neighbouring lanes hold neighbouring runs, so that each of the two loads
-// and stores covers whole stretches of the head (16 values in a row to a lane touch every line twice: 8192 tokens of 32/8
-// heads 41 to 44 us for 37, fp32 73 for 51).  Both values of a pair are in one lane: where they are neighbours they are in one
-// run; where i turns with i + rot_dim / 2 the first rot_lanes lanes have one run of each half, the others what does not turn.
-template <bool INTER>
-__device__ __forceinline__ int2 runs_of(int l, int rot_lanes) {
-  return INTER ? make_int2(8 * l, 64 + 8 * l) : l < rot_lanes ? make_int2(8 * l, 8 * (rot_lanes + l)) : make_int2(8 * (rot_lanes + l), 64 + 8 * l);
+// A lane holds two runs of 8 values of its head, in memory those that begin at 8 l and 64 + 8 l: each of the wave's loads and stores
+// covers whole lines (runs next to each other in a lane touch every line twice: 8192 tokens of 32/8 heads 41 to 44 us for 37,
+// fp32 73 for 51).  That has both values of a pair in one lane where they are neighbours or i turns with i + 64.  Where i turns
+// with i + rot_dim / 2 nearer by, the runs change lanes through LDS, there and back, and the first rot_lanes lanes
+// have one of each half, the others what does not turn (37.5 us, fp32 51 to 53, as with all dimensions; loaded and stored like
+// that 40 to 44, 55 to 69).
+__device__ __forceinline__ int2 paired_runs(int l, int rot_lanes) {
+  return l < rot_lanes ? make_int2(8 * l, 8 * (rot_lanes + l)) : make_int2(8 * (rot_lanes + l), 64 + 8 * l);
 }
 
 // Where the lane that turns it finds the cosine and sine of a pair: (j, l) of [4][8] entries of two pairs, the lane's own in entries j = 0..3.
 template <bool INTER>
 __device__ __forceinline__ int2 entry_of(int pair) {
   return INTER ? make_int2((pair >> 5) * 2 + ((pair >> 1) & 1), (pair & 31) >> 2) : make_int2((pair >> 1) & 3, pair >> 3);
+}
+
+// What lanes of a wave have written to LDS is there for its other lanes (they run in step, and LDS serves a wave in order).
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 // A lane's 16 values as they are in memory, two runs of 8.
@@ -147,6 +155,22 @@ struct Lane16 {
       u[1] = get16<STREAM>(x + 16);
       u[2] = get16<STREAM>(y);
       u[3] = get16<STREAM>(y + 16);
+    }
+  }
+  // through 128 values of LDS from the runs that the lane has to others
+  __device__ __forceinline__ void exchange(char* lds, int2 from, int2 to) {
+    constexpr int size = BF16 ? 2 : 4, n = BF16 ? 1 : 2;
+    wave_fence();
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      *(uint4*)(lds + from.x * size + 16 * i) = u[i];
+      *(uint4*)(lds + from.y * size + 16 * i) = u[n + i];
+    }
+    wave_fence();
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      u[i] = *(const uint4*)(lds + to.x * size + 16 * i);
+      u[n + i] = *(const uint4*)(lds + to.y * size + 16 * i);
     }
   }
   __device__ __forceinline__ void values(float* x) const {
@@ -235,7 +259,7 @@ __device__ __forceinline__ void turn16(float* x, const float4* cs, bool first_ru
 template <int MODE, bool BF16, bool INTER, int STREAM>
 __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
   constexpr bool kStreamLoads = STREAM >= 1, kStreamStores = STREAM >= 2;
-  extern __shared__ float4 lds_cs[][4][8];              // [wave and token] and what entry_of says
+  extern __shared__ float4 lds_cs[][4][8];              // [wave and token] and what entry_of says; behind that the heads whose runs change lanes
   const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * a.block_waves + threadIdx.x / 64);
   if (wave >= a.n_waves) return;
   const uint32_t group = div_by(wave, a.group_waves);
@@ -260,10 +284,12 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
   const int lane = threadIdx.x & 63, l = lane & 7;
   const int sub = (lane >> 3) >> (3 - deal.tokens_log2), g = (lane >> 3) & (at_once - 1);      // token and head of the lane
   const bool there = sub < tokens && h0 + g < deal.heads;
-  const int2 at = runs_of<INTER>(l, a.rot_lanes);
+  const int2 at = make_int2(8 * l, 64 + 8 * l);
   const float* weight = MODE == kMove ? nullptr : a.weight[kind];
   const bool any_turn = a.rot_lanes && kind != kV;
   const bool turns = any_turn && (INTER ? l < 2 * a.rot_lanes : l < a.rot_lanes), turns_too = INTER ? any_turn && l + 8 < 2 * a.rot_lanes : turns;
+  const bool swap = !INTER && any_turn && a.rot_lanes < 8;
+  const int2 runs = swap ? paired_runs(l, a.rot_lanes) : at;
 
   uint64_t step = 0;
   if (any_turn && lane < 8 * a.rot_lanes) step = a.steps[lane];
@@ -277,8 +303,8 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
   }
   float w[16];
   if (weight) {
-    __builtin_memcpy(w, weight + at.x, 32);
-    __builtin_memcpy(w + 8, weight + at.y, 32);
+    __builtin_memcpy(w, weight + runs.x, 32);
+    __builtin_memcpy(w + 8, weight + runs.y, 32);
   }
   if (MODE == kMove && (uint32_t)row_in >= (uint32_t)a.n_pool_rows) row_in = 0, row_out = -1;
   Lane16<BF16> raw;
@@ -295,12 +321,12 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
       cos_sin((uint64_t)(int64_t)a.pos[token0 + i] * step, c, s);
       ((float2*)&mine[i][e.x][e.y])[lane & 1] = make_float2(c * a.factor, s * a.factor);
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    wave_fence();
   }
   if (!there) return;
   uint4 lo, hi;
+  char* const head = (char*)(lds_cs + (a.block_waves << a.group_log2)) + threadIdx.x / 8 * (kHeadDim * (BF16 ? 2 : 4));
+  if (swap) raw.exchange(head, at, runs);
   if (BF16 && !weight && !any_turn) {       // values keep their bits
     lo = raw.u[0];
     hi = raw.u[1];
@@ -318,6 +344,12 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
     } else {
       lo = narrow(x);
       hi = narrow(x + 8);
+    }
+    if (swap) {
+      Lane16<true> y = {{lo, hi}};
+      y.exchange(head, runs, at);
+      lo = y.u[0];
+      hi = y.u[1];
     }
   }
   if (MODE != kMove && a.out[kind]) {
@@ -366,6 +398,7 @@ static tl_status launch(RowsArgs& a, const int32_t (&heads)[3], int32_t n, bool 
   // (moves of more than the cache are done sooner in workgroups of one wave: 131072 rows of 8 heads 182 us, in ones of four 192 to 197;
   // smaller ones, and the other calls, 0 to 4 % sooner in fours)
   a.block_waves = MODE == kMove && bytes >= kStreamAll ? 1 : kRowThreads / 64;
+  const size_t lds = a.block_waves * ((512 << a.group_log2) + (!interleaved && a.rot_lanes % 8 ? kWaveHeads * kHeadDim * (bf16 ? 2 : 4) : 0));
   // wave numbers stay below 2^25, and below 2^32 / waves for their quotient
   int64_t most = (1 << 25) / waves;
   if (most > ((int64_t)1 << 32) / waves / waves - 1) most = ((int64_t)1 << 32) / waves / waves - 1;
@@ -375,8 +408,7 @@ static tl_status launch(RowsArgs& a, const int32_t (&heads)[3], int32_t n, bool 
     a.first = done << a.group_log2;
     a.end = (done + m) << a.group_log2 < n ? (done + m) << a.group_log2 : n;
     a.n_waves = (uint32_t)(m * waves);
-    hipLaunchKernelGGL(kernel, dim3((a.n_waves + a.block_waves - 1) / a.block_waves), dim3(a.block_waves * 64), a.block_waves * 512 << a.group_log2,
-                       stream, a);
+    hipLaunchKernelGGL(kernel, dim3((a.n_waves + a.block_waves - 1) / a.block_waves), dim3(a.block_waves * 64), lds, stream, a);
   }
   TL_HIP(hipGetLastError());
   return TL_OK;
