@@ -374,9 +374,10 @@ tl_status tl_merge(tl_plan* plan, const float* out_partial, const float* lse, vo
 
 /* ------------------------------------------------------------------------------------
  * Rows between a layer's projection and the attention: norms of queries and keys for each head, position rotation, writes to
- * the pool, rows of the pool that move.  Every call enqueues one kernel (more than one where tokens times heads exceed 2^27)
- * and nothing else: no allocation, no copy, no state kept, so it may be captured into a HIP graph and runs on any stream.  A call of zero tokens
- * returns TL_OK at once and looks at no other argument.
+ * the pool, rows of the pool that move.  Every call enqueues one kernel (several in a row for very large calls: more than
+ * 2^27 heads of all tokens, or thousands of heads to a token) and nothing else: no allocation, no copy, no state kept, so it
+ * may be captured into a HIP graph and runs on any stream.  A call of zero tokens returns TL_OK at once and looks at no
+ * other argument.
  * ------------------------------------------------------------------------------------ */
 
 /* Position rotation.  Pair i of a head's first rot_dim values -- values i and i + rot_dim / 2, or with `interleaved` not 0 values

@@ -435,7 +435,7 @@ static Span dense_span(const void* p, int64_t n, int64_t heads) {
 }
 static bool meet(const Span& x, const Span& y) { return x.lo < y.hi && y.lo < x.hi; }
 
-// One input with its dense output (either may be absent), its strides in bytes; `span` its bytes.
+// One input with its dense output (either may be absent), its strides in elements.
 struct Rows {
   const char* name;
   const void* in;
