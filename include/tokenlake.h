@@ -398,7 +398,7 @@ tl_status tl_rope_steps(const double* inv_freq, int32_t n, uint64_t* steps_out);
 
 /* Rows of n tokens.  q: [n, q_heads, 128], k and v: [n, kv_heads, 128], device, bf16 if is_bf16 is not 0, else fp32; a token's heads
  * are head_stride elements apart, tokens row_stride, both of any size and sign (q, k and v may be views into one projection's
- * output), the 128 values of a head follow each other.  NULL: not there.
+ * output), the 128 values of a head follow each other.  NULL: not there.  Heads of what is there: 1 to 65536.
  * q_weight / k_weight: device fp32 [128] or NULL.  Given, each head of q / k is divided by the root of the mean of its squares
  * plus eps and multiplied by the weight, in front of the rotation; eps: positive, normal, looked at only then.
  * q_out / k_out / v_out: device, dense [n, heads, 128] bf16, rounded once from fp32; v is not changed but for that.  An

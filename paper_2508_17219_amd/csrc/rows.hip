@@ -16,13 +16,11 @@
 #include <type_traits>
 
 #include "attn_common.h"
+#include "rows_deal.h"
 
 namespace tl {
 
 constexpr int kRowThreads = 256;
-constexpr int kMostHeads = 1 << 16;
-constexpr int kWaveHeads = 8;            // heads that a wave takes at once: 8 lanes with 16 values each to a head
-constexpr int kMostTokensLog2 = 3;       // tokens that a wave has
 // What a call moves decides whether the 256 MB of cache in front of HBM are to keep it.  From 104 MiB on what is read makes room for
 // what is written; from 256 MiB on neither would be there when the attention reads it.  Between a producer and a reader of
 // all rows, with neither / loads / both passing by the cache: 67 MB 45.5 / 45.7 / 50 us, 134 MB 93.8 / 90.7 / 84, 201 MB 106 / 101 / 110,
@@ -31,19 +29,6 @@ constexpr int kMostTokensLog2 = 3;       // tokens that a wave has
 constexpr int64_t kStreamIn = (int64_t)104 << 20, kStreamAll = (int64_t)256 << 20;
 
 enum { kDense = 0, kToPool = 1, kMove = 2 };      // where rows come from and go to
-enum { kQ = 0, kK = 1, kV = 2 };
-
-// A quotient by a number that the host knows: n / d = n * magic >> 32 for n d < 2^32.
-struct Div {
-  uint32_t d, magic;
-};
-__device__ __forceinline__ uint32_t div_by(uint32_t n, Div x) { return x.d == 1 ? n : __umulhi(n, x.magic); }
-
-// How the heads of one kind are dealt to waves.  A wave takes 8 heads: of one token or, where there are at most 4 (2, 1), of 2 (4, 8) tokens.
-struct Deal {
-  int32_t heads, tokens_log2, waves;     // waves: that the tokens of a group have for this kind
-  Div per_tokens;                        // waves of 1 << tokens_log2 tokens
-};
 
 struct RowsArgs {
   const char* in[3];                     // queries, keys, values (kMove: the pool's keys and values)
@@ -51,15 +36,13 @@ struct RowsArgs {
   uint16_t* out[3];                      // dense, or null
   uint16_t* pool[3];                     // kToPool, kMove: where the rows named by dst go
   const float* weight[3];                // null: no norm
-  Deal deal[3];
+  Dealing dealing;
   const int32_t *src, *dst;              // rows of the pool; src: kMove
   const int32_t* pos;                    // positions (kMove: by how many they move)
   const uint64_t* steps;
   float eps, factor;
   int32_t n_pool_rows;
   int32_t rot_lanes;                     // rot_dim / 16: lanes of a head whose values turn; 0: no rotation
-  int32_t group_log2;                    // tokens that waves are counted for
-  Div group_waves;
   uint32_t n_waves, block_waves;
   int64_t first, end;                    // tokens of this launch
 };
@@ -262,24 +245,13 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
   extern __shared__ float4 lds_cs[][4][8];              // [wave and token] and what entry_of says; behind that the heads whose runs change lanes
   const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * a.block_waves + threadIdx.x / 64);
   if (wave >= a.n_waves) return;
-  const uint32_t group = div_by(wave, a.group_waves);
-  uint32_t part = wave - group * a.group_waves.d;
-  int kind = kQ;
-  if (part >= (uint32_t)a.deal[kQ].waves) {
-    part -= a.deal[kQ].waves;
-    kind = kK;
-    if (part >= (uint32_t)a.deal[kK].waves) {
-      part -= a.deal[kK].waves;
-      kind = kV;
-    }
-  }
-  const Deal deal = a.deal[kind];
-  const uint32_t tg = div_by(part, deal.per_tokens);
+  const Place place = place_of(a.dealing, wave);
+  const int kind = place.kind, h0 = place.head;
+  const Deal deal = a.dealing.kind[kind];
   const int at_once = kWaveHeads >> deal.tokens_log2;
-  const int64_t token0 = a.first + ((int64_t)group << a.group_log2) + ((int64_t)tg << deal.tokens_log2);
+  const int64_t token0 = a.first + place.token;
   if (token0 >= a.end) return;
   const int tokens = (int)min((int64_t)1 << deal.tokens_log2, a.end - token0);
-  const int h0 = (int)(part - tg * deal.per_tokens.d) * at_once;
 
   const int lane = threadIdx.x & 63, l = lane & 7;
   const int sub = (lane >> 3) >> (3 - deal.tokens_log2), g = (lane >> 3) & (at_once - 1);      // token and head of the lane
@@ -313,7 +285,7 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
     raw.template load<kStreamLoads>(in + (MODE == kMove ? row_in * a.row[kind] : token0 * a.row[kind] + sub * a.row[kind]), at);
   }
 
-  auto* const mine = lds_cs + ((threadIdx.x / 64) << a.group_log2);
+  auto* const mine = lds_cs + ((threadIdx.x / 64) << a.dealing.group_log2);
   if (any_turn) {
     const int2 e = entry_of<INTER>(lane);
     for (int i = 0; i < tokens; ++i) {
@@ -325,7 +297,7 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
   }
   if (!there) return;
   uint4 lo, hi;
-  char* const head = (char*)(lds_cs + (a.block_waves << a.group_log2)) + threadIdx.x / 8 * (kHeadDim * (BF16 ? 2 : 4));
+  char* const head = (char*)(lds_cs + (a.block_waves << a.dealing.group_log2)) + threadIdx.x / 8 * (kHeadDim * (BF16 ? 2 : 4));
   if (swap) raw.exchange(head, at, runs);
   if (BF16 && !weight && !any_turn) {       // values keep their bits
     lo = raw.u[0];
@@ -364,29 +336,10 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
   }
 }
 
-static Div div_of(uint32_t d) { return {d, d == 1 ? 0u : (uint32_t)(((uint64_t)1 << 32) / d) + 1u}; }
-
 // Deals the heads of queries, keys and values and launches; `bytes`: what the call reads and writes.
 template <int MODE>
 static tl_status launch(RowsArgs& a, const int32_t (&heads)[3], int32_t n, bool bf16, bool interleaved, int64_t bytes, hipStream_t stream) {
-  a.group_log2 = 0;
-  for (int i = 0; i < 3; ++i) {
-    Deal& d = a.deal[i];
-    d.heads = heads[i];
-    d.tokens_log2 = 0;
-    while (heads[i] && d.tokens_log2 < kMostTokensLog2 && heads[i] << (d.tokens_log2 + 1) <= kWaveHeads) ++d.tokens_log2;
-    if (d.tokens_log2 > a.group_log2) a.group_log2 = d.tokens_log2;
-  }
-  uint32_t waves = 0;
-  for (int i = 0; i < 3; ++i) {
-    Deal& d = a.deal[i];
-    const int32_t at_once = kWaveHeads >> d.tokens_log2;
-    const uint32_t per = heads[i] ? (uint32_t)(heads[i] + at_once - 1) / at_once : 1;
-    d.per_tokens = div_of(per);
-    d.waves = heads[i] ? (int32_t)(per << (a.group_log2 - d.tokens_log2)) : 0;
-    waves += d.waves;
-  }
-  a.group_waves = div_of(waves);
+  a.dealing = deal_heads(heads);
   const auto pick = [&](auto is_bf16, auto stream_mode) {
     return interleaved ? rows_kernel<MODE, is_bf16.value, true, stream_mode.value> : rows_kernel<MODE, is_bf16.value, false, stream_mode.value>;
   };
@@ -398,16 +351,14 @@ static tl_status launch(RowsArgs& a, const int32_t (&heads)[3], int32_t n, bool 
   // (moves of more than the cache are done sooner in workgroups of one wave: 131072 rows of 8 heads 182 us, in ones of four 192 to 197;
   // smaller ones, and the other calls, 0 to 4 % sooner in fours)
   a.block_waves = MODE == kMove && bytes >= kStreamAll ? 1 : kRowThreads / 64;
-  const size_t lds = a.block_waves * ((512 << a.group_log2) + (!interleaved && a.rot_lanes % 8 ? kWaveHeads * kHeadDim * (bf16 ? 2 : 4) : 0));
-  // wave numbers stay below 2^25, and below 2^32 / waves for their quotient
-  int64_t most = (1 << 25) / waves;
-  if (most > ((int64_t)1 << 32) / waves / waves - 1) most = ((int64_t)1 << 32) / waves / waves - 1;
-  const int64_t groups = ((int64_t)n + (1 << a.group_log2) - 1) >> a.group_log2;
+  const int32_t group_log2 = a.dealing.group_log2;
+  const size_t lds = a.block_waves * ((512 << group_log2) + (!interleaved && a.rot_lanes % 8 ? kWaveHeads * kHeadDim * (bf16 ? 2 : 4) : 0));
+  const int64_t most = most_groups(a.dealing), groups = ((int64_t)n + (1 << group_log2) - 1) >> group_log2;
   for (int64_t done = 0; done < groups; done += most) {
     const int64_t m = groups - done < most ? groups - done : most;
-    a.first = done << a.group_log2;
-    a.end = (done + m) << a.group_log2 < n ? (done + m) << a.group_log2 : n;
-    a.n_waves = (uint32_t)(m * waves);
+    a.first = done << group_log2;
+    a.end = (done + m) << group_log2 < n ? (done + m) << group_log2 : n;
+    a.n_waves = (uint32_t)(m * a.dealing.group_waves.d);
     hipLaunchKernelGGL(kernel, dim3((a.n_waves + a.block_waves - 1) / a.block_waves), dim3(a.block_waves * 64), lds, stream, a);
   }
   TL_HIP(hipGetLastError());

@@ -42,3 +42,20 @@ def test_rows_kernels_keep_everything_in_registers():
     assert len(kernels) == 30, kernels        # dense and to the pool: 2 types x 2 orders x 3 ways by the cache; moves: 2 x 3
     for name, registers, scratch in kernels:
         assert int(scratch) == 0 and int(registers) <= 64, (name, registers, scratch)        # 64: eight waves to a SIMD
+
+
+def test_every_head_is_dealt_to_one_wave_and_every_launch_takes_tokens(tmp_path):
+    """The dealing that the library launches by and the kernel finds its place by, over head counts up to the most that a call may have."""
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    if not os.path.exists(hipcc):
+        pytest.skip("no hipcc here")
+    exe = str(tmp_path / "tl_rows_deal")
+    cmd = [hipcc, "-O1", "-g", "-std=c++17", "--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+           "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined", "-Xarch_host", "-fno-sanitize-recover=undefined",
+           "-I", os.path.join(ROOT, "include"), "-I", os.path.join(ROOT, "paper_2508_17219_amd", "csrc"),
+           os.path.join(ROOT, "tests", "host_sanitize", "deal_driver.cpp"), "-o", exe]
+    build = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert build.returncode == 0, build.stdout[-3000:]
+    run = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=100)
+    assert run.returncode == 0, run.stdout[-3000:]
+    assert "every head dealt once" in run.stdout and "runtime error" not in run.stdout, run.stdout[-3000:]

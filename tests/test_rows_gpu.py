@@ -255,6 +255,31 @@ def test_rows_of_large_calls_are_the_rows_of_small_ones(mb, kind, norm):
         assert all(torch.equal(a, b) for a, b in zip(outs, again))
 
 
+@pytest.mark.parametrize("n,q_heads,kv_heads", [(2, 46337, 1), (3, 50000, 1), (61, 65536, 1), (2, 1, 23200), (3, 2, 65536), (1, 65536, 65536)])
+def test_rotate_rows_of_as_many_heads_as_there_may_be(n, q_heads, kv_heads):
+    """Tens of thousands of heads beside few (one token's, repeated): the calls return, and every token's rows are what a call of 8 heads gives."""
+    _say("%d tokens of %d/%d heads" % (n, q_heads, kv_heads))
+    freqs = _freqs(128)
+    rope, (qw, kw) = _rope(freqs), _weights(n)
+    pos = torch.arange(n, dtype=torch.int32, device=DEV) * 1009 + 5
+    few = _randn(q_heads, 8, 128)
+
+    def spread(heads):
+        return few.repeat(-(-heads // 8), 1)[:heads].view(1, heads, 128).expand(n, heads, 128)
+
+    outs = [_out(n, q_heads), _out(n, kv_heads), _out(n, kv_heads)]
+    B.tl_rotate_rows(rope, pos, spread(q_heads), spread(kv_heads), spread(kv_heads), *outs, qw, kw)
+    want_q, want_k = _out(n, 8), _out(n, 8)
+    eight = few.view(1, 8, 128).expand(n, 8, 128)
+    B.tl_rotate_rows(rope, pos, eight, eight, None, want_q, want_k, None, qw, kw)
+    for got, want, heads in zip(outs, (want_q, want_k, eight), (q_heads, kv_heads, kv_heads)):
+        for first in range(8):
+            part = got[:, first::8]
+            assert torch.equal(part, want[:, first:first + 1].expand(part.shape))
+    w, tol = ro.rows(_np(eight), pos.cpu().numpy(), freqs, weight=_np(qw))
+    _check(want_q, w, tol, "queries")
+
+
 # ---- the pool -----------------------------------------------------------------------------
 def _pool(n_slots, seg_len, kv_heads, seed=11):
     k, v = _randn(seed, n_slots, seg_len, kv_heads, 128), _randn(seed + 1, n_slots, seg_len, kv_heads, 128)
