@@ -184,20 +184,19 @@ __device__ __forceinline__ float squares(const Lane16<BF16>& raw, const float* x
 // The lane's 16 values over the root of the mean of the head's squares plus eps, times the lane's weights.
 template <bool BF16>
 __device__ __forceinline__ void norm16(const Lane16<BF16>& raw, float* x, float eps, const float* w) {
-  float ss = squares(raw, x);
-  // A sum of squares beyond 32 bits (rows that large mean that something is wrong upstream, but their norm is an ordinary number)
-  // is taken again of the values times 2^-70.
-  if (__builtin_expect(ss > 3.4e38f, 0)) {
-    ss = 0;
+  float mean = squares(raw, x) * (1.f / kHeadDim) + eps;
+  // Beyond 32 bits (rows that large mean that something is wrong upstream, but their norm is an ordinary number) it is taken again of
+  // the values times 2^-70 and eps times 2^-140.
+  if (__builtin_expect(mean > 3.4e38f, 0)) {
+    float ss = 0;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       x[i] *= 0x1p-70f;
       ss += x[i] * x[i];
     }
-    ss = sum8(ss);
-    eps = 0;
+    mean = sum8(ss) * (1.f / kHeadDim) + eps * 0x1p-70f * 0x1p-70f;
   }
-  const float r = __builtin_amdgcn_rsqf(ss * (1.f / kHeadDim) + eps);
+  const float r = __builtin_amdgcn_rsqf(mean);
 #pragma unroll
   for (int i = 0; i < 16; ++i) x[i] *= r * w[i];
 }

@@ -202,6 +202,20 @@ def test_rotate_rows_values_out_of_the_ordinary():
         assert torch.equal(vo, f.to(torch.bfloat16))
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("size,eps", [(2.0 ** 62, 1e38), (1e18, 3.4e38), (1e19, 3.4028234e38), (1e25, 3e38), (3e38, 3.4e38), (1e25, 1e-6), (1e-3, 1e30),
+                                      (2.0 ** -64, 2.0 ** -126), (2.0 ** -60, 2.0 ** -110), (0.0, 2.0 ** -126)])
+def test_the_norm_holds_for_every_eps(size, eps, kind):
+    """Any positive normal eps counts, beside squares beyond 32 bits and squares below the normal numbers too."""
+    _say("norm %s of %g with eps %g" % (kind, size, eps))
+    x = (_randn(17, 5, 3, 128, kind=torch.float32).clamp(-1, 1) * size).to(KIND[kind])
+    w = _weights(18)[0]
+    out = _out(5, 3)
+    B.tl_rotate_rows(None, None, x, q_out=out, q_weight=w, eps=eps)
+    want, tol = ro.rows(_np(x), None, weight=_np(w), eps=eps)
+    _check(out, want, tol, "norm")
+
+
 def test_rotate_rows_offsets_beyond_32_bits():
     """Tokens 2^31 values apart, and more tokens than one launch takes (their inputs one row, repeated)."""
     _say("long strides")
