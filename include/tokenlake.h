@@ -392,7 +392,7 @@ typedef struct tl_rope {
   float factor;
 } tl_rope;
 
-/* steps_out[i] = inv_freq[i] (radians per position) as a fraction of a turn times 2^64, modulo 2^64.  inv_freq, steps_out: host [n];
+/* steps_out[i] = inv_freq[i] (radians per position, of any size) as a fraction of a turn times 2^64, modulo 2^64, to the nearest.  inv_freq, steps_out: host [n];
  * TL_EINVAL for frequencies that are not finite.  Host arithmetic. */
 tl_status tl_rope_steps(const double* inv_freq, int32_t n, uint64_t* steps_out);
 

@@ -481,6 +481,34 @@ static tl_status launch_rows(const char* who, const tl_rope* rope, const tl_qkv*
   return launch<kToPool>(a, heads, n, d->is_bf16 != 0, interleaved, bytes, (hipStream_t)stream);
 }
 
+// 1 / 2 pi, from its first bit behind the point on.
+static const uint64_t kTurns[19] = {
+    0x28be60db9391054aull, 0x7f09d5f47d4d3770ull, 0x36d8a5664f10e410ull, 0x7f9458eaf7aef158ull, 0x6dc91b8e909374b8ull,
+    0x01924bba82746487ull, 0x3f877ac72c4a69cfull, 0xba208d7d4baed121ull, 0x3a671c09ad17df90ull, 0x4e64758e60d4ce7dull,
+    0x272117e2ef7e4a0eull, 0xc7fe25fff7816603ull, 0xfbcbc462d6829b47ull, 0xdb4d9fb3c9f2c26dull, 0xd3d18fd9a797fa8bull,
+    0x5d49eeb1faf97c5eull, 0xcf41ce7de294a4baull, 0x9afed7ec47e35742ull, 0x1580cc11bf1edaeaull};
+
+// 64 of its bits, those of weight 2^-(at + 1) and below.
+static uint64_t turns_bits(int at) {
+  if (at <= -64 || at >= 19 * 64) return 0;
+  if (at < 0) return kTurns[0] >> -at;
+  const int i = at / 64, r = at % 64;
+  return r == 0 ? kTurns[i] : kTurns[i] << r | (i + 1 < 19 ? kTurns[i + 1] >> (64 - r) : 0);
+}
+
+// Radians as a fraction of a turn times 2^64, modulo 2^64, to the nearest: |radians| = m 2^e with a whole m below 2^53, times those bits of
+// 2^(64 + e) / 2 pi that count: 64 in front of the point (m times the others is a multiple of 2^64) and 128 behind it (the others
+// are below 2^-75 together).  Payne and Hanek's reduction (Radian reduction for trigonometric functions, 1983), to turns in place of quarters.
+static uint64_t step_of(double radians) {
+  int e;
+  const uint64_t m = (uint64_t)ldexp(frexp(fabs(radians), &e), 53);
+  const int at = 64 + e - 53 - 64;
+  typedef unsigned __int128 u128;
+  const u128 low = (u128)m * turns_bits(at + 64) + (uint64_t)((u128)m * turns_bits(at + 128) >> 64);
+  const uint64_t step = m * turns_bits(at) + (uint64_t)(low >> 64) + ((uint64_t)low >> 63);
+  return radians < 0 ? 0 - step : step;
+}
+
 }  // namespace tl
 
 using namespace tl;
@@ -491,13 +519,7 @@ tl_status tl_rope_steps(const double* inv_freq, int32_t n, uint64_t* steps_out) 
   if (n < 0 || (n > 0 && (!inv_freq || !steps_out))) TL_FAIL(TL_EINVAL, "tl_rope_steps: bad argument");
   for (int32_t i = 0; i < n; ++i)
     if (!std::isfinite(inv_freq[i])) TL_FAIL(TL_EINVAL, "tl_rope_steps: frequency %d is not finite", i);
-  // (the host's long double has 64 bits of mantissa: the step is off by less than 2^-63 of itself)
-  const long double two_pi = 6.283185307179586476925286766559005768L;
-  for (int32_t i = 0; i < n; ++i) {
-    const long double turns = (long double)inv_freq[i] / two_pi, part = turns - floorl(turns);
-    const long double scaled = rintl(ldexpl(part, 64));
-    steps_out[i] = scaled >= 0x1p64L ? 0 : (uint64_t)scaled;
-  }
+  for (int32_t i = 0; i < n; ++i) steps_out[i] = step_of(inv_freq[i]);
   return TL_OK;
 }
 

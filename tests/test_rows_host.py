@@ -34,6 +34,35 @@ def test_steps_are_fractions_of_a_turn():
     assert B.load_library().tl_rope_steps(None, -1, None) == B.TL_EINVAL
 
 
+def _two_pi(bits):
+    """2 pi times 2^bits, by Machin's formula."""
+    def arctan_of_inverse(x):
+        power = total = (1 << (bits + 32)) // x
+        n = 1
+        while power:
+            power //= -x * x
+            n += 2
+            total += power // n
+        return total
+    return 8 * (4 * arctan_of_inverse(5) - arctan_of_inverse(239)) >> 32
+
+
+def test_steps_are_the_nearest_for_every_finite_frequency():
+    """Whole turns are taken off exactly, however many a position turns by: from the least number to the largest."""
+    two_pi = _two_pi(2400)
+    rng = np.random.default_rng(6)
+    bits = rng.integers(0, 2 ** 64, 4000, dtype=np.uint64).view(np.float64)
+    freqs = np.concatenate([[1.0, 7.5, -0.25, 123456.789, 1e300, -1e300, 1e22, 5e-324, 2.0 ** -1022, np.finfo(np.float64).max, 2 ** 53 + 2.0, 2.0 ** -60, 0.0, -0.0],
+                            rng.uniform(-1e6, 1e6, 500), 1e6 ** (-rng.random(500)), 2.0 ** np.arange(-1074, 1024), bits[np.isfinite(bits)]])
+    for f, step in zip(freqs.tolist(), B.tl_rope_steps(freqs).tolist()):
+        over, under = abs(f).as_integer_ratio()
+        scaled = (over << (64 + 64 + 2400)) // (under * two_pi)              # turns times 2^64, 64 bits behind the point (below 2^-1000 off)
+        want = (scaled if f >= 0 else -scaled) % (1 << 128)
+        off = abs((step << 64) - want)
+        off = min(off, (1 << 128) - off)
+        assert off <= (1 << 63) + 2, (f, step, off / 2 ** 64)
+
+
 # ---- places -------------------------------------------------------------------------------
 def test_reserved_rows_are_where_the_oracle_appends():
     rng = np.random.default_rng(3)
