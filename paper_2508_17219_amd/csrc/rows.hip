@@ -77,10 +77,11 @@ __device__ __forceinline__ uint4 narrow(const float* x) {
   return __builtin_bit_cast(uint4, pack_bf16x8(x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]));
 }
 
-// cos and sin of a phase (2^64 = one turn).  Quarter turns are taken off the integer; what is left, at most an eighth of a
-// turn, is exact to 2^-25 of itself, and the power series up to x^9 and x^8 are off by 2e-9 and 2.5e-8 there.
+// cos and sin of a phase (2^64 = one turn), rounded to 2^-32 of a turn: with the step's own 2^-65 times a position, what is turned by is off by at most
+// 2^-33 + 2^-34 of a turn.  Quarter turns are taken off the integer; what is left, at most an eighth of a turn, is exact to 3 x 2^-24 of itself
+// (the number, the constant and their product in 24 bits), and the power series up to x^9 and x^8 are off by 2e-9 and 2.5e-8 there.
 __device__ __forceinline__ void cos_sin(uint64_t phase, float& c, float& s) {
-  const uint32_t t = (uint32_t)(phase >> 32);
+  const uint32_t t = (uint32_t)(phase >> 32) + ((uint32_t)phase >> 31);
   const uint32_t quarter = (t + 0x20000000u) >> 30;
   const float x = (float)(int32_t)(t - (quarter << 30)) * 1.46291807926715968e-9f;      // 2 pi / 2^32
   const float z = x * x;

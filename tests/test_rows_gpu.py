@@ -126,6 +126,28 @@ def test_rotate_rows_at_every_position():
         _check(out, want, tol, "interleaved" if interleaved else "halves")
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotate_rows_angle_is_the_nearest_of_32_bits(interleaved):
+    """Angles of a few 2^-32 of a turn, which a sine shows to the bit: off by 2^-33 of a turn for the phase, and by what a sine of that size is rounded
+    by: half a step of bf16 (with what the first of two roundings adds), 2^-20 of it for 32 bits."""
+    _say("small angles, " + ("neighbours" if interleaved else "halves"))
+    parts = [0, 1, (1 << 31) - 1, 1 << 31, (1 << 31) + 1, (1 << 32) - 1]
+    steps = np.array([(j << 32) + f for j in (0, 1, 2, 3, 5, 9) for f in parts] + [0] * 28, np.uint64)
+    rope = B.tl_rope_of(torch.from_numpy(steps.view(np.int64)).to(DEV), interleaved)
+    positions = [1, -1, 2, -3]
+    x = torch.zeros(len(positions), 1, 128, device=DEV)
+    (x[..., 0::2] if interleaved else x[..., :64]).fill_(1)
+    out = _out(len(positions), 1)
+    B.tl_rotate_rows(rope, torch.tensor(positions, dtype=torch.int32, device=DEV), x, q_out=out)
+    got = _np(out)[:, 0]
+    got = got[:, 1::2] if interleaved else got[:, 64:]
+    turn = 2 * math.pi / 2.0 ** 32
+    want = np.array(positions)[:, None] * (steps.astype(np.float64) / 2.0 ** 32)[None] * turn
+    tol = 0.5 * turn + (np.abs(want) + 0.5 * turn) * (2.0 ** -8 * (1 + 2.0 ** -9) + 2.0 ** -20)
+    bad = np.abs(got - want) > tol
+    assert not bad.any(), (np.argwhere(bad)[0], got[bad][0] / turn, want[bad][0] / turn)
+
+
 def test_rotate_rows_strides_orders_and_starts():
     """Heads in front of tokens, tokens and heads that repeat (stride 0), tensors that start between 16-byte boundaries, outputs too."""
     _say("strides")
