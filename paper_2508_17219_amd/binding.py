@@ -8,8 +8,10 @@ host arrays are numpy arrays.  `stream=None` uses torch's current HIP stream.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from itertools import accumulate, chain
+from operator import mul
 from struct import Struct
 from typing import Optional
 
@@ -471,6 +473,26 @@ def _dense(t, name, kind, n, device):
     return t.data_ptr()
 
 
+def _in_order(shape, n, heads):
+    """Whether the elements of a dense tensor of this shape are those of [n, heads, 128] in that order: a flat one, leading dimensions of n tokens
+    or of n heads of all tokens, values last.  ([heads, n, 128] would be filled with tokens and heads mixed up.)"""
+    dims = [d for d in shape if d != 1]
+    return math.prod(dims) == n * heads * 128 and (
+        len(dims) < 2 or dims[-1] % 128 == 0 and (n == 1 or dims[0] == n * heads or n in accumulate(dims[:-1], mul)))
+
+
+def _out_of(t, name, bf16, n, heads, device):
+    """Address of a dense output [n, heads, 128], or of one of another shape with the same order."""
+    if t.dtype is not bf16:
+        raise TypeError("%s must be %s, is %s" % (name, bf16, t.dtype))
+    if t.get_device() != device:
+        raise ValueError("%s is on another device" % name)
+    shape = t.shape
+    if (shape != (n, heads, 128) and not _in_order(shape, n, heads)) or not t.is_contiguous():
+        raise ValueError("%s must be dense [%d, %d, 128], is %s with strides %s" % (name, n, heads, tuple(shape), t.stride()))
+    return t.data_ptr()
+
+
 # tl_qkv as bytes: filling the ctypes structure field by field takes 0.8 us, this 0.2
 _PACK_QKV = Struct("3Q6q3if5Q").pack
 
@@ -512,11 +534,11 @@ def _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps):
     if n > _MOST_ROWS:
         raise ValueError("%d tokens in one call" % n)
     if q_out is not None:
-        qo = _dense(q_out, "q_out", bf16, n * qh * 128, device)
+        qo = _out_of(q_out, "q_out", bf16, n, qh, device)
     if k_out is not None:
-        ko = _dense(k_out, "k_out", bf16, n * kh * 128, device)
+        ko = _out_of(k_out, "k_out", bf16, n, kh, device)
     if v_out is not None:
-        vo = _dense(v_out, "v_out", bf16, n * vh * 128, device)
+        vo = _out_of(v_out, "v_out", bf16, n, vh, device)
     if q_weight is not None:
         qw = _dense(q_weight, "q_weight", f32, 128, device)
     if k_weight is not None:
@@ -537,7 +559,8 @@ def _at(rope) -> Optional[int]:
 def tl_rotate_rows(rope: Optional[tl_rope], pos, q=None, k=None, v=None, q_out=None, k_out=None, v_out=None, q_weight=None, k_weight=None,
                    eps: float = 1e-6, stream=None):
     """Norms (with weights) and rotation (with rope) of q [n, q_heads, 128] and k [n, kv_heads, 128] with any strides between tokens and
-    heads, bf16 or fp32; v as it is; to dense bf16 tensors of as many elements.  pos: int32, n of them."""
+    heads, bf16 or fp32; v as it is; to dense bf16 tensors [n, heads, 128] (of any shape with that order: [n, heads * 128], [batch, length, heads, 128]).
+    pos: int32, n of them."""
     rows, at, n, _ = _qkv(rope, pos, q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps)
     _check(load_library().tl_rotate_rows(_at(rope), rows, at, n, _stream(stream)))
 

@@ -564,6 +564,31 @@ def test_binding_refuses_shapes_and_kinds():
     B.tl_pool_destroy(pool)
 
 
+def test_outputs_are_filled_in_the_order_that_their_shape_says():
+    """An output of another order ([heads, n, 128]: heads in front of tokens) is refused, each of the three; other shapes with the same order get the same bits."""
+    _say("orders of outputs")
+    n, hq, hkv = 10, 4, 2
+    q, k, v = _randn(1, n, hq, 128), _randn(2, n, hkv, 128), _randn(3, n, hkv, 128)
+    rope, pos = _rope(_freqs(128)), torch.arange(n, dtype=torch.int32, device=DEV)
+    want = [_out(n, hq), _out(n, hkv), _out(n, hkv)]
+    B.tl_rotate_rows(rope, pos, q, k, v, *want)
+    pool, pk, pv = _pool(2, 64, hkv)
+    for which, heads in enumerate((hq, hkv, hkv)):
+        for shape in ((heads, n, 128), (n, 128, heads), (heads, n * 128)):
+            outs = [_out(n, hq), _out(n, hkv), _out(n, hkv)]
+            outs[which] = torch.zeros(shape, dtype=torch.bfloat16, device=DEV)
+            with pytest.raises(ValueError, match="qkv"[which] + "_out"):
+                B.tl_rotate_rows(rope, pos, q, k, v, *outs)
+            with pytest.raises(ValueError, match="qkv"[which] + "_out"):
+                B.tl_pool_write_rows(pool, rope, pos, pos, k, v, q, *outs)
+        for shape in ((n, heads * 128), (1, n, heads * 128), (2, n // 2, heads, 128), (n * heads, 128), (n * heads * 128,)):
+            outs = [_out(n, hq), _out(n, hkv), _out(n, hkv)]
+            outs[which] = outs[which].view(shape)
+            B.tl_rotate_rows(rope, pos, q, k, v, *outs)
+            assert all(torch.equal(a.view(b.shape), b) for a, b in zip(outs, want))
+    B.tl_pool_destroy(pool)
+
+
 # ---- together, in front of the attention ---------------------------------------------------
 class _Model:
     """A layer's projections of sessions, and the norms and rotation that the oracle holds their rows to."""

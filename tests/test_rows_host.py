@@ -224,3 +224,16 @@ def test_binding_refuses_tensors_that_are_not_on_a_gpu():
     with pytest.raises(ValueError, match="device"):
         B.tl_pool_move_rows(pool, None, pos, pos)
     B.tl_pool_destroy(pool)
+
+
+@pytest.mark.parametrize("n,heads,fits,not_so", [
+    (10, 4, [(10, 4, 128), (10, 512), (5120,), (40, 128), (1, 10, 512), (2, 5, 4, 128), (2, 5, 512), (1, 40, 128), (10, 1, 512), (10, 2, 2, 128)],
+     [(4, 10, 128), (10, 128, 4), (128, 10, 4), (4, 1280), (2, 4, 5, 128), (4, 5, 2, 128), (20, 256), (10, 4, 64), (10, 4, 2, 128), (0, 4, 128)]),
+    (1, 4, [(1, 4, 128), (4, 1, 128), (512,), (4, 128), (1, 512)], [(128, 4), (1, 128, 4), (2, 4, 128)]),
+    (5, 1, [(5, 1, 128), (1, 5, 128), (640,), (5, 128)], [(128, 5), (128, 1, 5), (5, 1, 256)]),
+    (1, 1, [(1, 1, 128), (128,)], [(64, 2), ()])])
+def test_outputs_of_another_order_do_not_fit(n, heads, fits, not_so):
+    for shape in fits:
+        assert B._in_order(torch.Size(shape), n, heads), shape
+    for shape in not_so:
+        assert not B._in_order(torch.Size(shape), n, heads), shape
