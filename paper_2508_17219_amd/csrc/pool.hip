@@ -169,6 +169,18 @@ static int32_t take_slot(tl_pool* p, int32_t want) {
   return s < p->n_slots ? s : -1;
 }
 
+// Memory for the entries of ids that are about to be registered, or std::bad_alloc and none is there.
+static void enter_ids(tl_pool* p, const uint64_t* ids, int32_t n) {
+  int32_t entered = 0;
+  try {
+    for (; entered < n; ++entered) p->slot_of.emplace(ids[entered], -1);
+  } catch (...) {
+    while (entered > 0) p->slot_of.erase(ids[--entered]);
+    throw;
+  }
+}
+
+// Registers an id that enter_ids has entered.
 static void occupy(tl_pool* p, int32_t slot, uint64_t id, int32_t fill) {
   p->slot_of[id] = slot;
   p->id_of[slot] = id;
@@ -196,6 +208,11 @@ tl_status tl_pool_put(tl_pool* pool, uint64_t segment_id, const void* k_src_dev,
   if (want_slot >= 0 && pool->fill[want_slot] != 0) TL_FAIL(TL_EINVAL, "tl_pool_put: slot %d is taken", want_slot);
   int32_t s = take_slot(pool, want_slot);
   if (s < 0) TL_FAIL(TL_EFULL, "tl_pool_put: no free slot (%d in use)", pool->n_used);
+  try {
+    enter_ids(pool, &segment_id, 1);
+  } catch (const std::bad_alloc&) {
+    TL_FAIL(TL_ENOMEM, "tl_pool_put: host allocation failed");
+  }
   hipStream_t st = (hipStream_t)stream;
   // one launch: copy the fill rows, clear the rest of the slot
   const size_t row16 = (size_t)pool->kv_heads * pool->head_dim * 2 / 16;
@@ -206,7 +223,11 @@ tl_status tl_pool_put(tl_pool* pool, uint64_t segment_id, const void* k_src_dev,
   const unsigned bx = (unsigned)(slot16 / 256 > 32 ? 32 : (slot16 + 255) / 256);
   hipLaunchKernelGGL(append_rows_kernel, dim3(bx, 1), dim3(256), 0, st, (uint4*)pool->k_dev, (uint4*)pool->v_dev,
                      (const uint4*)k_src_dev, (const uint4*)v_src_dev, args, row16, slot16);
-  TL_HIP(hipGetLastError());
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) {
+    pool->slot_of.erase(segment_id);
+    TL_FAIL(TL_EHIP, "tl_pool_put: %s", hipGetErrorString(e));
+  }
   occupy(pool, s, segment_id, fill);
   if (slot_out) *slot_out = s;
   return TL_OK;
@@ -254,13 +275,7 @@ static tl_status place_rows(const char* who, tl_pool* pool, int32_t n_chains, co
 
   // ---- memory for all that is about to be entered, or nothing is ----
   chunks.reserve((size_t)n_chains + n_new_all);
-  int32_t entered = 0;
-  try {
-    for (; entered < n_new_all; ++entered) pool->slot_of.emplace(new_ids[entered], -1);
-  } catch (...) {
-    while (entered > 0) pool->slot_of.erase(new_ids[--entered]);
-    throw;
-  }
+  enter_ids(pool, new_ids, n_new_all);
 
   // ---- place the rows (host state changes from here on; no failure path below but HIP's) ----
   for (int32_t c = 0; c < n_chains; ++c) {
@@ -372,15 +387,20 @@ tl_status tl_pool_adopt(tl_pool* pool, const uint64_t* ids, const int32_t* slots
   (void)stream;
   if (!pool || n < 0 || (n > 0 && (!ids || !slots || !fills))) TL_FAIL(TL_EINVAL, "tl_pool_adopt: bad argument");
   // validate everything first so that a failure registers nothing
-  std::unordered_map<uint64_t, int> seen_id;
-  std::unordered_map<int32_t, int> seen_slot;
-  for (int32_t i = 0; i < n; ++i) {
-    if (slots[i] < 0 || slots[i] >= pool->n_slots) TL_FAIL(TL_EINVAL, "tl_pool_adopt: slot %d out of range", slots[i]);
-    if (fills[i] < 1 || fills[i] > pool->seg_len) TL_FAIL(TL_EINVAL, "tl_pool_adopt: fill %d outside 1..%d", fills[i], pool->seg_len);
-    if (pool->fill[slots[i]] != 0) TL_FAIL(TL_EINVAL, "tl_pool_adopt: slot %d is taken", slots[i]);
-    if (pool->slot_of.count(ids[i])) TL_FAIL(TL_EINVAL, "tl_pool_adopt: id %llu already resident", (unsigned long long)ids[i]);
-    if (!seen_id.emplace(ids[i], i).second) TL_FAIL(TL_EINVAL, "tl_pool_adopt: id %llu listed twice", (unsigned long long)ids[i]);
-    if (!seen_slot.emplace(slots[i], i).second) TL_FAIL(TL_EINVAL, "tl_pool_adopt: slot %d listed twice", slots[i]);
+  try {
+    std::unordered_map<uint64_t, int> seen_id;
+    std::unordered_map<int32_t, int> seen_slot;
+    for (int32_t i = 0; i < n; ++i) {
+      if (slots[i] < 0 || slots[i] >= pool->n_slots) TL_FAIL(TL_EINVAL, "tl_pool_adopt: slot %d out of range", slots[i]);
+      if (fills[i] < 1 || fills[i] > pool->seg_len) TL_FAIL(TL_EINVAL, "tl_pool_adopt: fill %d outside 1..%d", fills[i], pool->seg_len);
+      if (pool->fill[slots[i]] != 0) TL_FAIL(TL_EINVAL, "tl_pool_adopt: slot %d is taken", slots[i]);
+      if (pool->slot_of.count(ids[i])) TL_FAIL(TL_EINVAL, "tl_pool_adopt: id %llu already resident", (unsigned long long)ids[i]);
+      if (!seen_id.emplace(ids[i], i).second) TL_FAIL(TL_EINVAL, "tl_pool_adopt: id %llu listed twice", (unsigned long long)ids[i]);
+      if (!seen_slot.emplace(slots[i], i).second) TL_FAIL(TL_EINVAL, "tl_pool_adopt: slot %d listed twice", slots[i]);
+    }
+    enter_ids(pool, ids, n);
+  } catch (const std::bad_alloc&) {
+    TL_FAIL(TL_ENOMEM, "tl_pool_adopt: host allocation failed");
   }
   for (int32_t i = 0; i < n; ++i) occupy(pool, slots[i], ids[i], fills[i]);
   return TL_OK;

@@ -59,3 +59,20 @@ def test_every_head_is_dealt_to_one_wave_and_every_launch_takes_tokens(tmp_path)
     run = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=100)
     assert run.returncode == 0, run.stdout[-3000:]
     assert "every head dealt once" in run.stdout and "runtime error" not in run.stdout, run.stdout[-3000:]
+
+
+def test_host_memory_that_runs_out_registers_nothing(tmp_path):
+    """tl_pool_adopt, tl_pool_reserve_batch and tl_pool_put where the allocation of an entry fails: TL_ENOMEM, no exception, the pool as it was."""
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    if not os.path.exists(hipcc):
+        pytest.skip("no hipcc here")
+    exe = str(tmp_path / "tl_memory")
+    csrc = os.path.join(ROOT, "paper_2508_17219_amd", "csrc")
+    cmd = [hipcc, "-O1", "-g", "-std=c++17", "--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+           "-Xarch_host", "-fsanitize=undefined", "-Xarch_host", "-fno-sanitize-recover=undefined", "-I", os.path.join(ROOT, "include"), "-I", csrc,
+           os.path.join(ROOT, "tests", "host_sanitize", "memory_driver.cpp"), os.path.join(csrc, "pool.hip"), os.path.join(csrc, "prefix_tree.hip"), "-o", exe]
+    build = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert build.returncode == 0, build.stdout[-3000:]
+    run = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=100)
+    assert run.returncode == 0, run.stdout[-3000:]
+    assert "nothing registered" in run.stdout, run.stdout[-3000:]
