@@ -259,7 +259,7 @@ static tl_status place_rows(const char* who, tl_pool* pool, int32_t n_chains, co
         room[c] = C - pool->fill[tail_slot[c]];
       }
       const int32_t rest = n_rows > room[c] ? n_rows - room[c] : 0;
-      const int32_t need = (rest + C - 1) / C;
+      const int32_t need = (int32_t)(((int64_t)rest + C - 1) / C);
       if (n_new != need)
         TL_FAIL(TL_EINVAL, "%s: %d rows need exactly %d new segments, %d given", who, n_rows, need, n_new);
     }

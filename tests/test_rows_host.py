@@ -128,6 +128,17 @@ def test_reserve_refuses_what_append_refuses_and_changes_nothing():
     B.tl_pool_destroy(pool)
 
 
+def test_as_many_rows_as_there_may_be_are_counted():
+    """2^31 - 1 rows for a chain: the new segments that they need are told, without overflow."""
+    lib = B.load_library()
+    pool = B.tl_pool_create(4, 64, 1, 128, FAKE_K, FAKE_V)
+    none, new_ptr, row_ptr = np.zeros(1, np.int32), np.zeros(2, np.int32), np.array([0, 2 ** 31 - 1], np.int32)
+    rows = np.zeros(1, np.int32)
+    assert lib.tl_pool_reserve_batch(pool, 1, none.ctypes.data, None, new_ptr.ctypes.data, None, row_ptr.ctypes.data, None, rows.ctypes.data) == B.TL_EINVAL
+    assert b"need exactly 33554432 new segments" in lib.tl_last_error(), lib.tl_last_error()
+    B.tl_pool_destroy(pool)
+
+
 # ---- refusals -----------------------------------------------------------------------------
 def _rope(**kw):
     return B.tl_rope(**{**dict(steps_dev=0x5000, rot_dim=64, interleaved=0, factor=1.0), **kw})
