@@ -316,6 +316,79 @@ def test_rotate_rows_of_as_many_heads_as_there_may_be(n, q_heads, kv_heads):
     _check(want_q, w, tol, "queries")
 
 
+def _in_parts(rope, pos, q, k, v, qw, kw, part=2000):
+    """What tl_rotate_rows makes of the rows, by calls of a few tokens."""
+    outs = [None if t is None else torch.empty((t.shape[0], t.shape[1], 128), dtype=torch.bfloat16, device=DEV) for t in (q, k, v)]
+    for first in range(0, pos.shape[0], part):
+        at = slice(first, first + part)
+        B.tl_rotate_rows(rope, pos[at], *(None if t is None else t[at] for t in (q, k, v, *outs)), qw, kw)
+    return outs
+
+
+@pytest.mark.parametrize("rot,interleaved", [(128, False), (128, True), (96, False), (96, True), (0, False)])
+@pytest.mark.parametrize("mb,kind", [(70, "fp32"), (120, "bf16"), (120, "fp32"), (290, "bf16"), (290, "fp32")])
+def test_large_calls_of_every_order_are_small_ones(mb, kind, rot, interleaved):
+    """Both orders of pairs, all dimensions or some, both types, on each side of what the cache keeps: to the bits of small calls, every row."""
+    _say("%d MB %s rot %d %s" % (mb, kind, rot, interleaved))
+    q_heads, kv_heads = 9, 3
+    n = mb * 1000000 // ((q_heads + 2 * kv_heads) * 128 * (4 if kind == "bf16" else 6))
+    g = torch.Generator(device=DEV).manual_seed(mb + rot)
+    x = torch.randn(n, q_heads + 2 * kv_heads, 128, generator=g, device=DEV).to(KIND[kind])
+    q, k, v = x[:, :q_heads], x[:, q_heads:q_heads + kv_heads], x[:, q_heads + kv_heads:]
+    pos = torch.randint(0, 1 << 20, (n,), generator=g, device=DEV, dtype=torch.int32)
+    qw, kw = _weights(mb)
+    rope = _rope(_freqs(rot), interleaved, 1.1) if rot else None
+    outs = [torch.empty((n, h, 128), dtype=torch.bfloat16, device=DEV) for h in (q_heads, kv_heads, kv_heads)]
+    B.tl_rotate_rows(rope, pos, q, k, v, *outs, qw, kw)
+    assert all(torch.equal(a, b) for a, b in zip(outs, _in_parts(rope, pos, q, k, v, qw, kw)))
+    few = slice(n - 40, n)
+    for t, w, o in ((q, qw, outs[0]), (k, kw, outs[1])):
+        _check(o[few], *ro.rows(_np(t[few]), pos[few].cpu().numpy(), _freqs(rot) if rot else None, interleaved, 1.1 if rot else 1.0, _np(w)), "rows")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+def test_norms_of_rows_out_of_the_ordinary_in_both_types(kind):
+    """Infinities, NaN and squares beyond 32 bits, through the sum of squares of each type; no head disturbs another."""
+    _say("extremes of " + kind)
+    x = _randn(19, 7, 5, 128, kind=torch.float32)
+    x[1] *= 1e25
+    x[2] = 3e38
+    x[3, 1, 5] = float("inf")
+    x[3, 2, 127] = -float("inf")
+    x[4, 0, 64] = float("nan")
+    x[5, 3, :64] = -2e30
+    x[6, 4, 3], x[6, 4, 70] = float("inf"), float("nan")
+    x = x.to(KIND[kind])
+    w = _weights(20)[0]
+    out = _out(7, 5)
+    B.tl_rotate_rows(None, None, x, q_out=out, q_weight=w, eps=1e-6)
+    with np.errstate(invalid="ignore"):
+        want, tol = ro.rows(_np(x), None, weight=_np(w), eps=1e-6)
+    got, finite = _np(out), np.isfinite(_np(x)).all(-1)
+    assert finite.sum() == 7 * 5 - 4 and (np.abs(got - want) <= tol)[finite].all()
+    for token, head, at in ((3, 1, 5), (3, 2, 127)):
+        assert np.isnan(got[token, head, at]) and (np.delete(got[token, head], at) == 0).all()
+    assert np.isnan(got[4, 0]).all() and np.isnan(got[6, 4]).all()
+
+
+def test_rotate_rows_in_several_launches():
+    """16384 heads beside one: 112 tokens to a launch.  Three launches, the tokens on both sides of each border, queries, keys and values."""
+    _say("several launches")
+    n, q_heads, freqs = 250, 16384, _freqs(128)
+    rope, (qw, kw) = _rope(freqs), _weights(21)
+    pos = torch.arange(n, dtype=torch.int32, device=DEV) * 77 - 500
+    heads = torch.arange(q_heads, device=DEV) % 5
+    few = _randn(22, n, 5, 128)
+    q, k, v = _randn(23, 1, 5, 128)[:, heads].expand(n, q_heads, 128), few[:, :1], few[:, 1:2]
+    outs = [_out(n, q_heads, 1), _out(n, 1, 1), _out(n, 1, 1)]
+    B.tl_rotate_rows(rope, pos, q, k, v, *(o[:n] for o in outs), qw, kw)
+    want = _in_parts(rope, pos, _randn(23, 1, 5, 128).expand(n, 5, 128), k, v, qw, kw, part=7)
+    assert all(torch.equal(outs[0][at, :], want[0][at][heads]) for at in range(n))
+    assert torch.equal(outs[1][:n], want[1]) and torch.equal(outs[2][:n], v)
+    assert all(torch.isnan(o[n:].float()).all() for o in outs)
+    _check(want[0], *ro.rows(_np(_randn(23, 1, 5, 128).expand(n, 5, 128)), pos.cpu().numpy(), freqs, weight=_np(qw)), "queries")
+
+
 # ---- the pool -----------------------------------------------------------------------------
 def _pool(n_slots, seg_len, kv_heads, seed=11):
     k, v = _randn(seed, n_slots, seg_len, kv_heads, 128), _randn(seed + 1, n_slots, seg_len, kv_heads, 128)
@@ -460,6 +533,101 @@ def test_moves_of_many_rows_are_moves_of_a_few(kv_heads, seg_len, n):
     want, tol = ro.rows(_np(k0.view(-1, kv_heads, 128)[src[at].long()]), shift[at].cpu().numpy(), _freqs(128))
     _check(flat[dst[at].long()], want, tol, "keys")
     assert torch.equal(pv.view(-1, kv_heads, 128)[dst.long()], v0.view(-1, kv_heads, 128)[src.long()])
+    B.tl_pool_destroy(pool)
+
+
+@pytest.mark.parametrize("mb,kind,rot,interleaved,queries,dense", [
+    (60, "bf16", 96, False, True, True), (120, "bf16", 128, False, True, False), (120, "bf16", 64, True, False, True), (120, "fp32", 96, False, True, True),
+    (120, "fp32", 128, True, False, False), (300, "bf16", 96, False, True, True), (300, "bf16", 128, True, True, False), (300, "fp32", 128, False, False, True),
+    (300, "fp32", 64, True, True, True)])
+def test_large_writes_are_rotated_rows_at_their_places(mb, kind, rot, interleaved, queries, dense):
+    """Writes on each side of what the cache keeps: the pool's rows, all of them, and the outputs to the bits of small calls of tl_rotate_rows."""
+    _say("write %d MB %s rot %d %s" % (mb, kind, rot, interleaved))
+    q_heads, kv_heads, C = (5 if queries else 0), 3, 64
+    size = 2 if kind == "bf16" else 4
+    n = mb * 1000000 // (128 * (q_heads * (size + 2) + 2 * kv_heads * (size + 2 + (2 if dense else 0)))) + 1
+    g = torch.Generator(device=DEV).manual_seed(mb + rot)
+    x = torch.randn(n, q_heads + 2 * kv_heads, 128, generator=g, device=DEV).to(KIND[kind])
+    q, k, v = x[:, :q_heads] if queries else None, x[:, q_heads:q_heads + kv_heads], x[:, q_heads + kv_heads:]
+    pos = torch.randint(0, 1 << 20, (n,), generator=g, device=DEV, dtype=torch.int32)
+    qw, kw = _weights(mb)
+    rope = _rope(_freqs(rot), interleaved)
+    n_slots = n // C + 3
+    pk, pv = (torch.randn(n_slots, C, kv_heads, 128, generator=g, device=DEV, dtype=torch.bfloat16) for _ in "kv")
+    rows = torch.randperm(n_slots * C, generator=g, device=DEV)[:n].to(torch.int32)
+    rows[5] = -1
+    want_q, want_k, want_v = _in_parts(rope, pos, q, k, v, qw if queries else None, kw)
+    want_pk, want_pv = pk.clone(), pv.clone()
+    there = rows >= 0
+    want_pk.view(-1, kv_heads, 128)[rows[there].long()], want_pv.view(-1, kv_heads, 128)[rows[there].long()] = want_k[there], want_v[there]
+    pool = B.tl_pool_create(n_slots, C, kv_heads, 128, pk, pv)
+    outs = [_out(n, q_heads) if queries else None] + ([_out(n, kv_heads), _out(n, kv_heads)] if dense else [None, None])
+    B.tl_pool_write_rows(pool, rope, pos, rows, k, v, q, *outs, qw if queries else None, kw)
+    torch.cuda.synchronize()
+    assert torch.equal(pk, want_pk) and torch.equal(pv, want_pv)
+    assert all(a is None or torch.equal(a, b) for a, b in zip(outs, (want_q, want_k, want_v)))
+    B.tl_pool_destroy(pool)
+
+
+@pytest.mark.parametrize("n,rot,interleaved", [(20000, 64, False), (20000, 128, True), (33001, 64, False), (33001, 96, True), (33001, 112, False), (33001, 0, False)])
+def test_large_moves_of_every_order_are_moves_of_a_few(n, rot, interleaved):
+    """Some dimensions and neighbouring pairs on both sides of the cache's size, a part of the rows in place."""
+    _say("move %d rows rot %d %s" % (n, rot, interleaved))
+    kv_heads, C = 8, 64
+    n_slots = 2 * n // C + 2
+    g = torch.Generator(device=DEV).manual_seed(n + rot)
+    pk, pv = (torch.randn(n_slots, C, kv_heads, 128, generator=g, device=DEV, dtype=torch.bfloat16) for _ in "kv")
+    k0, v0 = pk.clone(), pv.clone()
+    pool = B.tl_pool_create(n_slots, C, kv_heads, 128, pk, pv)
+    order = torch.randperm(n_slots * C, generator=g, device=DEV).to(torch.int32)
+    src, dst = order[:n].contiguous(), order[n:2 * n].contiguous()
+    dst[::7] = src[::7]
+    shift = torch.randint(-5000, 5000, (n,), generator=g, device=DEV, dtype=torch.int32) if rot else None
+    rope = _rope(_freqs(rot), interleaved) if rot else None
+    B.tl_pool_move_rows(pool, rope, src, dst, shift)
+    big_k, big_v = pk.clone(), pv.clone()
+    pk.copy_(k0), pv.copy_(v0)
+    for first in range(0, n, 1000):
+        part = slice(first, first + 1000)
+        B.tl_pool_move_rows(pool, rope, src[part], dst[part], None if shift is None else shift[part])
+    assert torch.equal(pk, big_k) and torch.equal(pv, big_v)
+    flat = lambda t: t.view(-1, kv_heads, 128)  # noqa: E731
+    at = torch.tensor([0, 1, 7, n // 2, n - 1], device=DEV)
+    want, tol = ro.rows(_np(flat(k0)[src[at].long()]), np.zeros(5) if shift is None else shift[at].cpu().numpy(), _freqs(rot) if rot else None, interleaved)
+    _check(flat(pk)[dst[at].long()], want, tol, "keys")
+    assert torch.equal(flat(pv)[dst.long()], flat(v0)[src.long()])
+    B.tl_pool_destroy(pool)
+
+
+def test_writes_and_moves_in_several_launches():
+    """A pool of 32768 heads: 63 tokens to a launch.  70 rows are written and moved, and those of neighbouring places stay."""
+    _say("several launches to the pool")
+    kv_heads, C, n = 32768, 64, 70
+    freqs = _freqs(128)
+    rope, kw = _rope(freqs), _weights(24)[1]
+    pk = torch.zeros(3, C, kv_heads, 128, dtype=torch.bfloat16, device=DEV)
+    pv = torch.zeros_like(pk)
+    pool = B.tl_pool_create(3, C, kv_heads, 128, pk, pv)
+    flat_k, flat_v = pk.view(-1, kv_heads, 128), pv.view(-1, kv_heads, 128)
+    heads = torch.arange(kv_heads, device=DEV) % 5
+    one_k, one_v = _randn(25, 1, 5, 128), _randn(26, 1, 5, 128)
+    pos, rows = torch.arange(n, dtype=torch.int32, device=DEV) * 13, torch.arange(n, dtype=torch.int32, device=DEV) + 1
+    rows[64] = -1
+    B.tl_pool_write_rows(pool, rope, pos, rows, one_k[:, heads].expand(n, kv_heads, 128), one_v[:, heads].expand(n, kv_heads, 128), k_weight=kw)
+    want = _in_parts(rope, pos, None, one_k.expand(n, 5, 128), None, None, kw)[1]
+    for i in range(n):
+        if i != 64:
+            assert torch.equal(flat_k[i + 1], want[i][heads]) and torch.equal(flat_v[i + 1], one_v[0][heads]), i
+    assert not flat_k[0].any() and not flat_k[65].any() and not flat_k[n + 1:].any() and not flat_v[65].any()
+    # to places behind them, the last row in place
+    src = torch.arange(n, dtype=torch.int32, device=DEV) + 1
+    dst = torch.arange(n, dtype=torch.int32, device=DEV) + 100
+    dst[69] = src[69]
+    B.tl_pool_move_rows(pool, rope, src, dst, torch.full_like(src, 1000))
+    turned = _in_parts(rope, torch.full_like(src, 1000), None, want, None, None, None)[1]
+    for i in (0, 1, 61, 62, 63, 65, 68, 69):
+        assert torch.equal(flat_k[dst[i].long()], turned[i][heads]) and torch.equal(flat_v[dst[i].long()], one_v[0][heads]), i
+    assert not flat_k[164].any() and not flat_k[0].any() and not flat_v[99].any()
     B.tl_pool_destroy(pool)
 
 
