@@ -36,13 +36,15 @@ struct RowsArgs {
   uint16_t* out[3];                      // dense, or null
   uint16_t* pool[3];                     // kToPool, kMove: where the rows named by dst go
   const float* weight[3];                // null: no norm
-  Dealing dealing;
+  Deal deal[3];
   const int32_t *src, *dst;              // rows of the pool; src: kMove
   const int32_t* pos;                    // positions (kMove: by how many they move)
   const uint64_t* steps;
   float eps, factor;
   int32_t n_pool_rows;
   int32_t rot_lanes;                     // rot_dim / 16: lanes of a head whose values turn; 0: no rotation
+  int32_t group_log2;                    // tokens that waves are counted for
+  Div group_waves;
   uint32_t n_waves, block_waves;
   int64_t first, end;                    // tokens of this launch
 };
@@ -245,9 +247,9 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
   extern __shared__ float4 lds_cs[][4][8];              // [wave and token] and what entry_of says; behind that the heads whose runs change lanes
   const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * a.block_waves + threadIdx.x / 64);
   if (wave >= a.n_waves) return;
-  const Place place = place_of(a.dealing, wave);
+  const Place place = place_of(a.deal, a.group_log2, a.group_waves, wave);
+  const Deal deal = place.deal;
   const int kind = place.kind, h0 = place.head;
-  const Deal deal = a.dealing.kind[kind];
   const int at_once = kWaveHeads >> deal.tokens_log2;
   const int64_t token0 = a.first + place.token;
   if (token0 >= a.end) return;
@@ -285,7 +287,7 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
     raw.template load<kStreamLoads>(in + (MODE == kMove ? row_in * a.row[kind] : token0 * a.row[kind] + sub * a.row[kind]), at);
   }
 
-  auto* const mine = lds_cs + ((threadIdx.x / 64) << a.dealing.group_log2);
+  auto* const mine = lds_cs + ((threadIdx.x / 64) << a.group_log2);
   if (any_turn) {
     const int2 e = entry_of<INTER>(lane);
     for (int i = 0; i < tokens; ++i) {
@@ -297,7 +299,7 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
   }
   if (!there) return;
   uint4 lo, hi;
-  char* const head = (char*)(lds_cs + (a.block_waves << a.dealing.group_log2)) + threadIdx.x / 8 * (kHeadDim * (BF16 ? 2 : 4));
+  char* const head = (char*)(lds_cs + (a.block_waves << a.group_log2)) + threadIdx.x / 8 * (kHeadDim * (BF16 ? 2 : 4));
   if (swap) raw.exchange(head, at, runs);
   if (BF16 && !weight && !any_turn) {       // values keep their bits
     lo = raw.u[0];
@@ -339,7 +341,10 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(const RowsArgs a) {
 // Deals the heads of queries, keys and values and launches; `bytes`: what the call reads and writes.
 template <int MODE>
 static tl_status launch(RowsArgs& a, const int32_t (&heads)[3], int32_t n, bool bf16, bool interleaved, int64_t bytes, hipStream_t stream) {
-  a.dealing = deal_heads(heads);
+  const Dealing dealing = deal_heads(heads);
+  for (int i = 0; i < 3; ++i) a.deal[i] = dealing.kind[i];
+  a.group_log2 = dealing.group_log2;
+  a.group_waves = dealing.group_waves;
   const auto pick = [&](auto is_bf16, auto stream_mode) {
     return interleaved ? rows_kernel<MODE, is_bf16.value, true, stream_mode.value> : rows_kernel<MODE, is_bf16.value, false, stream_mode.value>;
   };
@@ -351,14 +356,13 @@ static tl_status launch(RowsArgs& a, const int32_t (&heads)[3], int32_t n, bool 
   // (moves of more than the cache are done sooner in workgroups of one wave: 131072 rows of 8 heads 182 us, in ones of four 192 to 197;
   // smaller ones, and the other calls, 0 to 4 % sooner in fours)
   a.block_waves = MODE == kMove && bytes >= kStreamAll ? 1 : kRowThreads / 64;
-  const int32_t group_log2 = a.dealing.group_log2;
-  const size_t lds = a.block_waves * ((512 << group_log2) + (!interleaved && a.rot_lanes % 8 ? kWaveHeads * kHeadDim * (bf16 ? 2 : 4) : 0));
-  const int64_t most = most_groups(a.dealing), groups = ((int64_t)n + (1 << group_log2) - 1) >> group_log2;
+  const size_t lds = a.block_waves * ((512 << a.group_log2) + (!interleaved && a.rot_lanes % 8 ? kWaveHeads * kHeadDim * (bf16 ? 2 : 4) : 0));
+  const int64_t most = most_groups(dealing), groups = ((int64_t)n + (1 << a.group_log2) - 1) >> a.group_log2;
   for (int64_t done = 0; done < groups; done += most) {
     const int64_t m = groups - done < most ? groups - done : most;
-    a.first = done << group_log2;
-    a.end = (done + m) << group_log2 < n ? (done + m) << group_log2 : n;
-    a.n_waves = (uint32_t)(m * a.dealing.group_waves.d);
+    a.first = done << a.group_log2;
+    a.end = (done + m) << a.group_log2 < n ? (done + m) << a.group_log2 : n;
+    a.n_waves = (uint32_t)(m * a.group_waves.d);
     hipLaunchKernelGGL(kernel, dim3((a.n_waves + a.block_waves - 1) / a.block_waves), dim3(a.block_waves * 64), lds, stream, a);
   }
   TL_HIP(hipGetLastError());

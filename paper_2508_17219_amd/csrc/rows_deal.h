@@ -74,24 +74,25 @@ inline int64_t most_groups(const Dealing& a) {
 // What wave number `wave` of a launch has: heads from `head` on of one kind, of up to 1 << tokens_log2 tokens from the launch's number `token` on.
 struct Place {
   int kind;
+  Deal deal;                             // the kind's
   int64_t token;
   int head;
 };
-__host__ __device__ __forceinline__ Place place_of(const Dealing& a, uint32_t wave) {
-  const uint32_t group = div_by(wave, a.group_waves);
-  uint32_t part = wave - group * a.group_waves.d;
+__host__ __device__ __forceinline__ Place place_of(const Deal (&deal)[3], int32_t group_log2, const Div& group_waves, uint32_t wave) {
+  const uint32_t group = div_by(wave, group_waves);
+  uint32_t part = wave - group * group_waves.d;
   int kind = kQ;
-  if (part >= (uint32_t)a.kind[kQ].waves) {
-    part -= a.kind[kQ].waves;
+  if (part >= (uint32_t)deal[kQ].waves) {
+    part -= deal[kQ].waves;
     kind = kK;
-    if (part >= (uint32_t)a.kind[kK].waves) {
-      part -= a.kind[kK].waves;
+    if (part >= (uint32_t)deal[kK].waves) {
+      part -= deal[kK].waves;
       kind = kV;
     }
   }
-  const Deal& d = a.kind[kind];
+  const Deal d = deal[kind];
   const uint32_t tg = div_by(part, d.per_tokens);
-  return {kind, ((int64_t)group << a.group_log2) + ((int64_t)tg << d.tokens_log2), (int)(part - tg * d.per_tokens.d) * (kWaveHeads >> d.tokens_log2)};
+  return {kind, d, ((int64_t)group << group_log2) + ((int64_t)tg << d.tokens_log2), (int)(part - tg * d.per_tokens.d) * (kWaveHeads >> d.tokens_log2)};
 }
 
 }  // namespace tl

@@ -32,7 +32,7 @@ static void deal(int32_t q, int32_t k, int32_t v) {
     if (g >= most) continue;
     seen.assign(seen.size(), 0);
     for (int64_t w = g * waves; w < (g + 1) * waves; ++w) {
-      const Place p = place_of(a, (uint32_t)w);
+      const Place p = place_of(a.kind, a.group_log2, a.group_waves, (uint32_t)w);
       check(p.kind >= 0 && p.kind < 3 && heads[p.kind] > 0, "a wave of a kind that is not there", heads);
       const Deal& d = a.kind[p.kind];
       const int at_once = kWaveHeads >> d.tokens_log2;
