@@ -22,10 +22,16 @@ namespace tl {
 
 constexpr int kRowThreads = 256;
 // What a call moves decides whether the 256 MB of cache in front of HBM are to keep it.  From 104 MiB on what is read makes room for
-// what is written; from 256 MiB on neither would be there when the attention reads it.  Between a producer and a reader of
-// all rows, with neither / loads / both passing by the cache: 67 MB 45.5 / 45.7 / 50 us, 134 MB 93.8 / 90.7 / 84, 201 MB 106 / 101 / 110,
-// 258 MB 150 / 131 / 135, 302 MB 182 / 157 / 155, 470 MB 253 / 266 / 236; alone 14.4 / 16.3 / 14.3, 29 / 27 / 25, 38.8 / 36.8 / 35.2, 48 / 48 / 44,
-// 55 / 55 / 51, 84 / 87 / 79.
+// what is written; from 256 MiB on neither would be there when the attention reads it.  us with neither / loads / both passing by the cache
+// (rotations of 32/8 heads with norms, 15 blocks of each in turn, which differ by 1 to 4 %), alone and with a copy of other rows to the call's
+// inputs in front of it and one of its outputs behind it, both timed with it:
+//    67 MB  13.6 / 14.6 / 14.3    39.6 / 38.1 / 39.9        201 MB  37.2 / 34.8 / 34.7    111 / 105 / 107
+//    90 MB  17.2 / 17.6 / 17.7    50.8 / 50.1 / 53.7        230 MB  42.6 / 40.8 / 39.1    130 / 119 / 124
+//   110 MB  21.2 / 20.4 / 20.7    61.1 / 58.7 / 63.2        258 MB  47.3 / 45.7 / 43.4    150 / 134 / 136
+//   134 MB  26.1 / 24.6 / 24.1    73.2 / 69.9 / 74.9        302 MB  54.6 / 53.2 / 50.2    180 / 158 / 158
+//   165 MB  31.4 / 28.8 / 29.2    91.1 / 86.0 / 89.2        470 MB  82.1 / 81.5 / 76.5    261 / 268 / 248
+// Loads alone are first between the copies from 67 to 258 MB and from 110 MB on do not lose to neither by themselves; both are
+// 4 to 6 % ahead by themselves from 230 MB on and first between the copies behind 302.
 constexpr int64_t kStreamIn = (int64_t)104 << 20, kStreamAll = (int64_t)256 << 20;
 
 enum { kDense = 0, kToPool = 1, kMove = 2 };      // where rows come from and go to
@@ -353,8 +359,10 @@ static tl_status launch(RowsArgs& a, const int32_t (&heads)[3], int32_t n, bool 
                                : bytes >= kStreamIn ? pick(is_bf16, std::integral_constant<int, 1>()) : pick(is_bf16, std::integral_constant<int, 0>());
   };
   const auto kernel = bf16 || MODE == kMove ? pick_stream(std::true_type()) : pick_stream(std::bool_constant<MODE == kMove>());
-  // (moves of more than the cache are done sooner in workgroups of one wave: 131072 rows of 8 heads 182 us, in ones of four 192 to 197;
-  // smaller ones, and the other calls, 0 to 4 % sooner in fours)
+  // (workgroups of one wave for moves of more than the cache: 131072 rows of 8 heads 179 us, in ones of four 200; 65536 90 and 95; 33000, the first
+  // behind the line, 46.3 and 46.8.  Below it 24000 rows 35.2 and 36.4, 16000 24.2 and 25.7, 8000 and fewer the same within 3 %: fours there too, for
+  // one line with the stores' way.  Rotations and writes of 1 to 8000 tokens and of 100 to 470 MB are the same within 4 % but for 16 tokens, 2.9 and
+  // 3.1, and writes of 200 MB, 31.8 and 33.9: fours.)
   a.block_waves = MODE == kMove && bytes >= kStreamAll ? 1 : kRowThreads / 64;
   const size_t lds = a.block_waves * ((512 << a.group_log2) + (!interleaved && a.rot_lanes % 8 ? kWaveHeads * kHeadDim * (bf16 ? 2 : 4) : 0));
   const int64_t most = most_groups(dealing), groups = ((int64_t)n + (1 << a.group_log2) - 1) >> a.group_log2;
