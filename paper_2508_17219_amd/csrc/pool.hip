@@ -421,9 +421,13 @@ tl_status tl_pool_evict_lru(tl_pool* pool, uint64_t* evicted_id) {
   for (int32_t s = 0; s < pool->n_slots; ++s)
     if (pool->fill[s] != 0 && pool->refcnt[s] == 0 && (best < 0 || pool->stamp[s] < pool->stamp[best])) best = s;
   if (best < 0) TL_FAIL(TL_ENOTFOUND, "tl_pool_evict_lru: no segment with zero references");
+  try {
+    pool->tree.remove_slot(best);        // a prefix that has lost a segment is no prefix: its nodes go, with what hangs below
+  } catch (const std::bad_alloc&) {
+    TL_FAIL(TL_ENOMEM, "tl_pool_evict_lru: host allocation failed");
+  }
   if (evicted_id) *evicted_id = pool->id_of[best];
   pool->slot_of.erase(pool->id_of[best]);
-  pool->tree.remove_slot(best);          // a prefix that has lost a segment is no prefix: its nodes go, with what hangs below
   pool->fill[best] = 0;
   pool->n_used--;
   pool->generation++;

@@ -36,14 +36,15 @@ int32_t PrefixTree::child(int32_t parent, uint64_t id, int32_t slot) {
   }
   auto it = child_of_.find(Key{parent, id});
   if (it != child_of_.end()) return it->second;
-  int32_t n;
-  if (!free_.empty()) {
-    n = free_.back();
-    free_.pop_back();
-  } else {
-    n = (int32_t)nodes_.size();
+  // (what allocates comes first: where it throws, nothing names the node; the list of free nodes has room for all, so that unlink does not)
+  if (free_.empty()) {
     nodes_.emplace_back();
+    free_.reserve(nodes_.capacity());
+    free_.push_back((int32_t)nodes_.size() - 1);
   }
+  const int32_t n = free_.back();
+  child_of_.emplace(Key{parent, id}, n);
+  free_.pop_back();
   TreeNode& x = nodes_[n];
   x = TreeNode{};
   x.id = id;
@@ -62,7 +63,6 @@ int32_t PrefixTree::child(int32_t parent, uint64_t id, int32_t slot) {
   x.next_same_slot = slot_head_[slot];
   if (x.next_same_slot >= 0) nodes_[x.next_same_slot].prev_same_slot = n;
   slot_head_[slot] = n;
-  child_of_.emplace(Key{parent, id}, n);
   ++live_;
   return n;
 }

@@ -1,4 +1,4 @@
-// Host memory that runs out while ids are entered into the pool: every call says TL_ENOMEM, nothing throws across the C boundary and nothing is
+// Host memory that runs out while ids are entered into the pool or leave it: every call says TL_ENOMEM, nothing throws across the C boundary and nothing is
 // registered.  operator new fails at the n-th call for every n until the call gets through.  Device pointers are fake; no call here enqueues work.
 #include <cstdint>
 #include <cstdio>
@@ -6,6 +6,7 @@
 #include <new>
 #include <vector>
 
+#include "tl_internal.h"
 #include "tokenlake.h"
 
 static long g_left = -1;       // allocations until one fails; -1: none does
@@ -90,6 +91,55 @@ int main() {
     check_unchanged(pool, 1, ids);
     CHECK(tl_pool_fills(pool, &slot, 1, &now) == TL_OK && now == fill);
     CHECK(tl_pool_destroy(pool) == TL_OK);
+    ++failures;
+  }
+
+  // prefix tree and eviction: paths 1000, 1001, ... under the root and the same ids under 1005, so that slots have nodes with and without children
+  for (long n = 0;; ++n) {
+    tl_pool* pool = new_pool();
+    CHECK(tl_pool_adopt(pool, ids.data(), slots.data(), fills.data(), 40, nullptr) == TL_OK);
+    for (uint64_t id : ids) CHECK(tl_pool_release(pool, id) == TL_OK);
+    bool threw = false;
+    int32_t at = 0, made = 0;
+    g_left = n;
+    try {
+      for (int i = 0; i < 40; ++i) at = pool->tree.child(i % 8 ? at : 0, ids[i], slots[i]), ++made;
+      for (int i = 0; i < 40; ++i)
+        if (i != 5) pool->tree.child(i % 3 ? at : pool->tree.child(0, ids[5], slots[5]), ids[i], slots[i]);
+    } catch (const std::bad_alloc&) {
+      threw = true;
+    }
+    g_left = -1;
+    const int32_t before = pool->tree.size();
+    // every node is reached from the root and from its parent by its id
+    std::vector<int32_t> order;
+    pool->tree.level_order(1 << 20, order);
+    CHECK((int32_t)order.size() == before && before >= made);
+    for (int32_t x : order) CHECK(pool->tree.child(pool->tree.at(x).parent, pool->tree.at(x).id, pool->tree.at(x).slot) == x);
+    // evictions with one failure each, until all is gone
+    uint64_t gone = 0;
+    int32_t used = 40;
+    while (used > 0) {
+      g_left = n % 3;
+      tl_status s = tl_pool_evict_lru(pool, &gone);
+      g_left = -1;
+      int32_t now = 0;
+      CHECK(tl_pool_used(pool, &now) == TL_OK);
+      if (s == TL_ENOMEM) {
+        CHECK(now == used);
+        ++failures;
+        s = tl_pool_evict_lru(pool, &gone);
+        CHECK(tl_pool_used(pool, &now) == TL_OK);
+      }
+      CHECK(s == TL_OK && now == used - 1);
+      used = now;
+      order.clear();
+      pool->tree.level_order(1 << 20, order);
+      CHECK((int32_t)order.size() == pool->tree.size());
+    }
+    CHECK(pool->tree.size() == 0);
+    CHECK(tl_pool_destroy(pool) == TL_OK);
+    if (!threw) break;
     ++failures;
   }
 

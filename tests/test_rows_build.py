@@ -62,7 +62,7 @@ def test_every_head_is_dealt_to_one_wave_and_every_launch_takes_tokens(tmp_path)
 
 
 def test_host_memory_that_runs_out_registers_nothing(tmp_path):
-    """tl_pool_adopt, tl_pool_reserve_batch and tl_pool_put where the allocation of an entry fails: TL_ENOMEM, no exception, the pool as it was."""
+    """tl_pool_adopt, tl_pool_reserve_batch, tl_pool_put, tl_pool_evict_lru and the prefix tree where an allocation fails: TL_ENOMEM, no exception, the pool as it was."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     if not os.path.exists(hipcc):
         pytest.skip("no hipcc here")
