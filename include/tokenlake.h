@@ -29,7 +29,7 @@
  *    other argument (empty tensors have null pointers).
  *  - A plan holds slot numbers and fills as they were when it was built.  Any change to the
  *    pool's slots afterwards (tl_pool_put of a new id, tl_pool_append, tl_pool_append_batch,
- *    tl_pool_adopt, tl_pool_evict_lru) makes it stale: tl_segment_attn and tl_fused_attn then
+ *    tl_pool_reserve_batch, tl_pool_adopt, tl_pool_evict_lru) makes it stale: tl_segment_attn and tl_fused_attn then
  *    return TL_EINVAL and enqueue nothing; build a new plan (Section 3.2: plans are made per
  *    iteration).  tl_pool_release and a put of a resident id change no slot and keep plans valid.
  *    A plan may outlive its pool only to be destroyed or read back (info, export, hot slots).
@@ -392,8 +392,8 @@ typedef struct tl_rope {
   float factor;
 } tl_rope;
 
-/* steps_out[i] = inv_freq[i] (radians per position, of any size) as a fraction of a turn times 2^64, modulo 2^64, to the nearest.  inv_freq, steps_out: host [n];
- * TL_EINVAL for frequencies that are not finite.  Host arithmetic. */
+/* steps_out[i] = inv_freq[i] (radians per position, of any size) as a fraction of a turn times 2^64, modulo 2^64, to the nearest.
+ * inv_freq, steps_out: host [n]; TL_EINVAL for frequencies that are not finite.  Host arithmetic. */
 tl_status tl_rope_steps(const double* inv_freq, int32_t n, uint64_t* steps_out);
 
 /* Rows of n tokens.  q: [n, q_heads, 128], k and v: [n, kv_heads, 128], device, bf16 if is_bf16 is not 0, else fp32; a token's heads

@@ -1206,7 +1206,7 @@ tl_status plan_device_ready(tl_plan* p, hipStream_t stream) {
 tl_status plan_is_current(const tl_plan* plan, const tl_pool* pool, const char* who) {
   if (plan->pool != pool) TL_FAIL(TL_EINVAL, "%s: plan was built for another pool", who);
   if (plan->pool_generation != pool->generation)
-    TL_FAIL(TL_EINVAL, "%s: the pool has changed since the plan was built (put, append, adopt or evict): build a new plan", who);
+    TL_FAIL(TL_EINVAL, "%s: the pool has changed since the plan was built (put, append, reserve, adopt or evict): build a new plan", who);
   return TL_OK;
 }
 

@@ -128,6 +128,20 @@ def test_reserve_refuses_what_append_refuses_and_changes_nothing():
     B.tl_pool_destroy(pool)
 
 
+def test_a_plan_goes_stale_when_rows_are_reserved():
+    """A tail that grows alone, and a new segment: a plan made before is refused in front of any device work, and names the reason."""
+    lib = B.load_library()
+    for tails, ids, counts in (([10], [[]], [3]), ([None], [[12]], [5])):
+        pool = B.tl_pool_create(4, 64, 1, 128, FAKE_K, FAKE_V)
+        B.tl_pool_adopt(pool, [10, 11], [0, 1], [20, 64])
+        plan = B.tl_plan_create(pool, 1, [0, 3], [0, 2], np.array([11, 10], np.uint64), B.TL_PLAN_SELF_BLOCK)
+        B.tl_pool_reserve_batch(pool, tails, ids, counts)
+        assert lib.tl_segment_attn(pool, plan, FAKE_K, 0.1, FAKE_K, FAKE_V, None) == B.TL_EINVAL
+        assert b"pool has changed" in lib.tl_last_error() and b"reserve" in lib.tl_last_error()
+        B.tl_plan_destroy(plan)
+        B.tl_pool_destroy(pool)
+
+
 def test_as_many_rows_as_there_may_be_are_counted():
     """2^31 - 1 rows for a chain: the new segments that they need are told, without overflow."""
     lib = B.load_library()
